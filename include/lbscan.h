@@ -212,6 +212,109 @@ int lbscan_conv1d_fwd(const lbscan_conv_args *args, void *hip_stream);
 int lbscan_conv1d_bwd(const lbscan_conv_args *fwd_args, const void *dy,
                       void *dx, float *dweight, float *dbias, void *hip_stream);
 
+/* ---- Operators of recurrent sequence models around the scan ------------------------
+ * Storage types, ownership, streams and errors as above.  Sums, states and statistics are
+ * fp32 whatever dtype says; every output is overwritten and every sum is added in a fixed order (the
+ * same bits on every run).  Tensors are dense, aligned to their element type (a 2-byte tensor may
+ * start at any element), and outputs do not overlap inputs unless a comment says so. */
+
+/* Gated linear recurrence along the last axis of (B,D,L), in the order of the tokens:
+ *     a_t = exp(-rate softplus(decay[d]) sigma(gate_a[b,d,t]))      sigma: the logistic function
+ *     h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigma(gate_x[b,d,t]) x[b,d,t],   h_{-1} = h0 or 0
+ *     y_t = h_t
+ * starts[b,t] != 0: a new sequence begins at token t (sequences packed into one row): h_{t-1}
+ * counts as zero there, whatever it is.  reverse = 1: the tokens are taken from the last to the first; the state
+ * enters at t = L-1 and leaves after t = 0. */
+typedef struct lbscan_gated_args {
+    int32_t batch, dim, seqlen;   /* B, D, L; any may be 0 (L = 0: the state passes through).
+                                     L <= 2^28, B * D < 2^31 */
+    int32_t dtype;                /* storage type of x, gate_a, gate_x, y and their gradients */
+    int32_t reverse;              /* 0/1 */
+    float rate;                   /* finite, >= 0 */
+    const void    *x;             /* (B,D,L) */
+    const void    *gate_a;        /* (B,D,L) before the logistic function */
+    const void    *gate_x;        /* (B,D,L) before the logistic function */
+    const float   *decay;         /* (D) */
+    const uint8_t *starts;        /* (B,L), 0 or not, or NULL: one sequence a row */
+    const float   *h0;            /* (B,D) or NULL: zeros */
+    void          *y;             /* (B,D,L) out (not read by the backward call) */
+    float         *hT;            /* (B,D) out, or NULL: not wanted.  May be h0 itself (a state
+                                     updated in place) */
+    void          *workspace;     /* lbscan_gated_workspace_bytes(args, LBSCAN_WS_FWD / _BWD) */
+    size_t         workspace_bytes;
+    void          *saved_state;   /* optional, LBSCAN_WS_SAVED bytes: states that the forward call
+                                     leaves for the backward call; NULL: computed again */
+    size_t         saved_state_bytes;
+} lbscan_gated_args;
+
+int lbscan_gated_fwd(const lbscan_gated_args *args, void *hip_stream);
+
+/* Gradients of lbscan_gated_fwd.  dout is the gradient of y, dhT (nullable) that of the state that
+ * leaves.  dx, dgate_a, dgate_x (B,D,L), ddecay (D); dh0 (B,D) nullable.  All are finite also
+ * where a gate is closed and sqrt(1 - a^2) has no derivative: the products have limits there.
+ * fwd_args->y and hT are not read. */
+int lbscan_gated_bwd(const lbscan_gated_args *fwd_args, const void *dout, const float *dhT,
+                     void *dx, void *dgate_a, void *dgate_x, float *ddecay, float *dh0,
+                     void *hip_stream);
+
+/* which: LBSCAN_WS_FWD, LBSCAN_WS_BWD (less when saved_state is given) or LBSCAN_WS_SAVED. */
+size_t lbscan_gated_workspace_bytes(const lbscan_gated_args *args, int which);
+
+/* Layer norm of the rows of (rows, dim):
+ *     s = x + residual (x itself without one)
+ *     y = (s - mean(s)) / sqrt(mean((s - mean(s))^2) + eps) * weight + bias
+ * The residual stream is fp32 and so is the sum, which the next norm takes as its residual. */
+typedef struct lbscan_norm_args {
+    int64_t rows;                 /* 0: only zeros are written to dweight, dbias */
+    int32_t dim;                  /* 0: nothing is computed; <= 2^23 */
+    int32_t dtype;                /* storage type of x, y and their gradients */
+    float eps;                    /* finite, >= 0 */
+    const void  *x;               /* (rows, dim).  Backward: read without a residual only */
+    const float *residual;        /* (rows, dim) or NULL.  Backward: only whether there is one */
+    const float *weight;          /* (dim) or NULL: ones */
+    const float *bias;            /* (dim) or NULL: zeros */
+    void        *y;               /* (rows, dim) out; may be x itself.  Not read by the backward call */
+    float       *sum;             /* (rows, dim), with a residual: out of the forward call (may be
+                                     residual itself), read by the backward call */
+    float       *mean, *rstd;     /* (rows) both out of the forward call, or both NULL: not wanted; read by
+                                     the backward call */
+    void        *workspace;       /* backward: lbscan_norm_workspace_bytes() */
+    size_t       workspace_bytes;
+} lbscan_norm_args;
+
+int lbscan_norm_fwd(const lbscan_norm_args *args, void *hip_stream);
+
+/* Gradients of lbscan_norm_fwd.  dout is the gradient of y, dsum (fp32, nullable, with a residual only)
+ * that of sum.  dx and, with a residual, dresidual (fp32) receive the same values in their types; with a
+ * residual either may be NULL.  dweight and dbias (dim) may each be NULL: not wanted. */
+int lbscan_norm_bwd(const lbscan_norm_args *fwd_args, const void *dout, const float *dsum,
+                    void *dx, float *dresidual, float *dweight, float *dbias, void *hip_stream);
+
+size_t lbscan_norm_workspace_bytes(const lbscan_norm_args *args);
+
+/* Token embedding: out[i,:] = scale weight[ids[i],:], zeros where ids[i] is outside [0, vocab) (padding).
+ * The gradient: dweight[v,:] = scale * the sum of dout[i,:] over the tokens i with ids[i] = v, the whole table
+ * written (zeros for rows that no token has). */
+#define LBSCAN_IDS_INT32 0
+#define LBSCAN_IDS_INT64 1
+typedef struct lbscan_embed_args {
+    int64_t tokens;               /* < 2^31 - 2^16; 0: only zeros are written to dweight */
+    int32_t vocab, dim;           /* vocab >= 1 where there are tokens; dim <= 2^23 */
+    int32_t dtype;                /* storage type of weight, out and their gradients */
+    int32_t ids_type;             /* LBSCAN_IDS_* */
+    float scale;
+    const void *ids;              /* (tokens) */
+    const void *weight;           /* (vocab, dim).  Not read by the backward call */
+    void       *out;              /* (tokens, dim) */
+    void       *workspace;        /* backward: lbscan_embed_workspace_bytes() */
+    size_t      workspace_bytes;
+} lbscan_embed_args;
+
+int lbscan_embed_fwd(const lbscan_embed_args *args, void *hip_stream);
+int lbscan_embed_bwd(const lbscan_embed_args *fwd_args, const void *dout, void *dweight,
+                     void *hip_stream);
+size_t lbscan_embed_workspace_bytes(const lbscan_embed_args *args);
+
 /* Bytes of device scratch the call named by `which` (LBSCAN_WS_*) needs for
  * these sizes; 0 means workspace may be NULL. */
 size_t lbscan_workspace_bytes(const lbscan_args *args, int which);

@@ -23,6 +23,9 @@ EXPORTS = (
     "lbscan_default_window", "lbscan_strerror", "lbscan_last_error", "lbscan_version",
     "lbscan_set_option", "lbscan_bwd_state", "lbscan_conv1d_fwd", "lbscan_conv1d_bwd",
     "lbscan_fwd_static",
+    "lbscan_gated_fwd", "lbscan_gated_bwd", "lbscan_gated_workspace_bytes",
+    "lbscan_norm_fwd", "lbscan_norm_bwd", "lbscan_norm_workspace_bytes",
+    "lbscan_embed_fwd", "lbscan_embed_bwd", "lbscan_embed_workspace_bytes",
 )
 
 
@@ -51,6 +54,40 @@ class LbscanConvArgs(ctypes.Structure):
         ("reverse", ctypes.c_int32),
         ("x", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
         ("y", ctypes.c_void_p),
+    ]
+
+
+class LbscanGatedArgs(ctypes.Structure):
+    """Mirror of struct lbscan_gated_args."""
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("dim", ctypes.c_int32), ("seqlen", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("reverse", ctypes.c_int32), ("rate", ctypes.c_float),
+        ("x", ctypes.c_void_p), ("gate_a", ctypes.c_void_p), ("gate_x", ctypes.c_void_p),
+        ("decay", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("h0", ctypes.c_void_p),
+        ("y", ctypes.c_void_p), ("hT", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("saved_state", ctypes.c_void_p), ("saved_state_bytes", ctypes.c_size_t),
+    ]
+
+
+class LbscanNormArgs(ctypes.Structure):
+    """Mirror of struct lbscan_norm_args."""
+    _fields_ = [
+        ("rows", ctypes.c_int64), ("dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+        ("x", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+        ("bias", ctypes.c_void_p), ("y", ctypes.c_void_p), ("sum", ctypes.c_void_p),
+        ("mean", ctypes.c_void_p), ("rstd", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class LbscanEmbedArgs(ctypes.Structure):
+    """Mirror of struct lbscan_embed_args."""
+    _fields_ = [
+        ("tokens", ctypes.c_int64), ("vocab", ctypes.c_int32), ("dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("ids_type", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("ids", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("out", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
     ]
 
 
@@ -92,6 +129,15 @@ def load():
     lib.lbscan_conv1d_fwd.argtypes = [cp, vp]
     lib.lbscan_conv1d_bwd.restype = ctypes.c_int
     lib.lbscan_conv1d_bwd.argtypes = [cp] + [vp] * 5
+    for name, struct_type, tensors in (("gated", LbscanGatedArgs, 7), ("norm", LbscanNormArgs, 6),
+                                       ("embed", LbscanEmbedArgs, 2)):
+        sp = ctypes.POINTER(struct_type)
+        fwd, bwd, size = (getattr(lib, f"lbscan_{name}_{what}") for what in ("fwd", "bwd", "workspace_bytes"))
+        fwd.restype = bwd.restype = ctypes.c_int
+        fwd.argtypes = [sp, vp]
+        bwd.argtypes = [sp] + [vp] * (tensors + 1)
+        size.restype = ctypes.c_size_t
+        size.argtypes = [sp, ctypes.c_int] if name == "gated" else [sp]
     lib.lbscan_workspace_bytes.restype = ctypes.c_size_t
     lib.lbscan_workspace_bytes.argtypes = [ap, ctypes.c_int]
     lib.lbscan_default_window.restype = ctypes.c_int

@@ -14,11 +14,19 @@ namespace {
 
 thread_local char g_last_error[256] = "";
 
+}  // namespace
+
+namespace lbscan {
 int hip_fail(hipError_t e, const char* where)
 {
     snprintf(g_last_error, sizeof(g_last_error), "%s: %s", where, hipGetErrorString(e));
     return LBSCAN_EHIP;
 }
+}  // namespace lbscan
+
+namespace {
+
+using lbscan::hip_fail;
 
 // Scratch missing or too small; for the fixed array the text says what was asked for.
 int scratch_too_small(size_t need, size_t have, bool fixed)

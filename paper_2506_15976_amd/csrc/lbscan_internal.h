@@ -8,6 +8,9 @@
 
 namespace lbscan {
 
+// Keeps the text of a HIP error for lbscan_last_error(); LBSCAN_EHIP.
+int hip_fail(hipError_t e, const char* where);
+
 // Arguments of one forward launch, already validated by the C entry points.
 struct FwdParams {
     int batch, dim, dstate, seqlen;

@@ -1,0 +1,512 @@
+// Layer norm and its gradient (formulas: lbscan_norm.h).
+//
+// A row is held in the registers of a team (16 lanes, a wave, or the waves of a block): it is read once, its
+// mean and then the mean of the squared deviations are summed over the team (two passes over registers, so no
+// difference of large numbers), and it is written once.  A team walks several rows with weight and bias (backward: the
+// sums of their gradients) of its columns in registers, the next row's loads in flight.
+#include "lbscan_device.h"
+#include "lbscan_internal.h"
+#include "lbscan_norm.h"
+
+namespace lbscan {
+namespace {
+
+// E consecutive elements, at any element's address.
+template <typename T, int E> struct __attribute__((packed, aligned(sizeof(T)))) Pack { T v[E]; };
+
+template <typename T, int E>
+__device__ __forceinline__ void get(const T* __restrict__ p, float out[E])
+{
+    const Pack<T, E> q = *reinterpret_cast<const Pack<T, E>*>(p);
+#pragma unroll
+    for (int e = 0; e < E; ++e) out[e] = to_f32(q.v[e]);
+}
+template <typename T, int E>
+__device__ __forceinline__ void put(T* __restrict__ p, const float in[E])
+{
+    Pack<T, E> q;
+#pragma unroll
+    for (int e = 0; e < E; ++e) q.v[e] = from_f32<T>(in[e]);
+    *reinterpret_cast<Pack<T, E>*>(p) = q;
+}
+
+template <int CTRL>
+__device__ __forceinline__ float turned(float v)
+{
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float lane_of(float v, int lane)
+{
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
+}
+// Sum over 16 lanes (G = 16) or a wave (G = 64), the same in every lane.
+template <int G>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    v += turned<0x128>(v);                                        // row_ror 8, 4, 2, 1
+    v += turned<0x124>(v);
+    v += turned<0x122>(v);
+    v += turned<0x121>(v);
+    if constexpr (G == 64) v = (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+    return v;
+}
+// The same over the W waves of a block; `slot` is not used again before another barrier.
+template <int G, int W>
+__device__ __forceinline__ float team_sum(float v, float (*slot)[W])
+{
+    v = lanes_sum<G>(v);
+    if constexpr (W > 1) {
+        if ((threadIdx.x & 63) == 0) (*slot)[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) v += (*slot)[w];
+    }
+    return v;
+}
+
+// Columns of a lane: NV packs of E.  The last pack of a row that E does not divide ends with the row; the
+// columns that the pack before it holds too count once in the sums (`in`) and are written twice with the
+// same value.
+template <int E>
+struct Columns {
+    int col, own;           // first column loaded, first one that counts
+    __device__ __forceinline__ Columns(int pack, int dim)
+    {
+        own = pack * E;
+        col = min(own, dim - E);
+    }
+    __device__ __forceinline__ bool in(int e, int dim) const { return col + e >= own && own < dim; }
+};
+
+template <int G, int W, int P> struct NormTeam {          // P: elements of a lane
+    static constexpr int kThreads = W == 1 ? 256 : 64 * W;
+    static constexpr int kRows = W == 1 ? 4 * (64 / G) : 1;       // rows of a block at a time
+    static constexpr int kLanes = G * W;
+    // the next row is loaded before the present one is worked on, where there are registers for it
+    static constexpr bool kAhead = P <= 16;
+};
+
+template <typename T, bool RES, int E, int G, int W, int NV>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_fwd_kernel(const NormParams p)
+{
+    using Team = NormTeam<G, W, E * NV>;
+    __shared__ float slots[4][W];
+    const int dim = p.dim;
+    const int member = W == 1 ? threadIdx.x & (G - 1) : threadIdx.x;
+    const int team = W > 1 ? 0 : G == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x / G;
+    const float scale = 1.0f / (float)dim;
+    // all packs are whole and inside the row
+    const bool whole = dim == Team::kLanes * E * NV;
+
+    float w[NV][E], b[NV][E];
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const Columns<E> at(c * Team::kLanes + member, dim);
+#pragma unroll
+        for (int e = 0; e < E; ++e) { w[c][e] = 1.0f; b[c][e] = 0.0f; }
+        if (p.weight) get<float, E>(p.weight + at.col, w[c]);
+        if (p.bias) get<float, E>(p.bias + at.col, b[c]);
+    }
+    const long step = (long)gridDim.x * Team::kRows;
+    long row = (long)blockIdx.x * Team::kRows + team;
+    Pack<T, E> qx[NV];
+    Pack<float, E> qr[NV];
+    auto fetch = [&](long r) {
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const Columns<E> at(c * Team::kLanes + member, dim);
+            qx[c] = *reinterpret_cast<const Pack<T, E>*>(static_cast<const T*>(p.x) + r * dim + at.col);
+            if constexpr (RES) qr[c] = *reinterpret_cast<const Pack<float, E>*>(p.residual + r * dim + at.col);
+        }
+    };
+    if (Team::kAhead && row < p.rows) fetch(row);
+    for (int parity = 0; row < p.rows; row += step, parity ^= 2) {
+        if (!Team::kAhead) fetch(row);
+        float s[NV][E];
+        float sum = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                s[c][e] = to_f32(qx[c].v[e]);
+                if constexpr (RES) s[c][e] += qr[c].v[e];
+            }
+        if (Team::kAhead && row + step < p.rows) fetch(row + step);
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const Columns<E> at(c * Team::kLanes + member, dim);
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum += whole || at.in(e, dim) ? s[c][e] : 0.0f;
+        }
+        const float mean = team_sum<G, W>(sum, &slots[parity]) / (float)dim;     // (exact for constant rows)
+        float square = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const Columns<E> at(c * Team::kLanes + member, dim);
+            // (not before the team has met: in place, the columns of a last pack that others hold too would
+            // be loaded by them with the sum already in them)
+            if constexpr (RES) put<float, E>(p.sum + row * dim + at.col, s[c]);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                s[c][e] -= mean;
+                square += whole || at.in(e, dim) ? s[c][e] * s[c][e] : 0.0f;
+            }
+        }
+        const float rstd = 1.0f / sqrtf(team_sum<G, W>(square, &slots[parity + 1]) * scale + p.eps);
+        if (p.mean && member == 0) { p.mean[row] = mean; p.rstd[row] = rstd; }
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const Columns<E> at(c * Team::kLanes + member, dim);
+            float o[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = fmaf(s[c][e] * rstd, w[c][e], b[c][e]);
+            put<T, E>(static_cast<T*>(p.y) + row * dim + at.col, o);
+        }
+    }
+}
+
+template <typename T, bool RES, int E, int G, int W, int NV>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_bwd_kernel(const NormParams p)
+{
+    using Team = NormTeam<G, W, E * NV>;
+    using S = std::conditional_t<RES, float, T>;
+    __shared__ float slots[2][2][W];
+    __shared__ float fold[W == 1 && G == 64 ? 3 * 64 * NV * E * 2 : 1];
+    const int dim = p.dim;
+    const int member = W == 1 ? threadIdx.x & (G - 1) : threadIdx.x;
+    const int team = W > 1 ? 0 : G == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x / G;
+    const float scale = 1.0f / (float)dim;
+    const bool whole = dim == Team::kLanes * E * NV;
+    const S* s_in = RES ? reinterpret_cast<const S*>(p.sum) : static_cast<const S*>(p.x);
+
+    float w[NV][E], dw[NV][E], db[NV][E];
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const Columns<E> at(c * Team::kLanes + member, dim);
+#pragma unroll
+        for (int e = 0; e < E; ++e) { w[c][e] = 1.0f; dw[c][e] = 0.0f; db[c][e] = 0.0f; }
+        if (p.weight) get<float, E>(p.weight + at.col, w[c]);
+    }
+    const long step = (long)gridDim.x * Team::kRows;
+    long row = (long)blockIdx.x * Team::kRows + team;
+    Pack<S, E> qs[NV];
+    Pack<T, E> qy[NV];
+    Pack<float, E> qd[NV];
+    float mean = 0.0f, rstd = 0.0f;
+    auto fetch = [&](long r) {
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const Columns<E> at(c * Team::kLanes + member, dim);
+            qs[c] = *reinterpret_cast<const Pack<S, E>*>(s_in + r * dim + at.col);
+            qy[c] = *reinterpret_cast<const Pack<T, E>*>(static_cast<const T*>(p.dy) + r * dim + at.col);
+            if constexpr (RES && Team::kAhead)
+                if (p.dsum) qd[c] = *reinterpret_cast<const Pack<float, E>*>(p.dsum + r * dim + at.col);
+        }
+        mean = p.mean[r];
+        rstd = p.rstd[r];
+    };
+    if (Team::kAhead && row < p.rows) fetch(row);
+    for (int parity = 0; row < p.rows; row += step, parity ^= 1) {
+        if (!Team::kAhead) fetch(row);
+        float hat[NV][E], g[NV][E], d[NV][E];
+        float sum_g = 0.0f, sum_gh = 0.0f;
+        const float rs = rstd;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const Columns<E> at(c * Team::kLanes + member, dim);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const bool in = whole || at.in(e, dim);
+                const float dy = to_f32(qy[c].v[e]);
+                hat[c][e] = (to_f32(qs[c].v[e]) - mean) * rs;
+                g[c][e] = dy * w[c][e];
+                if (Team::kAhead) d[c][e] = RES && p.dsum ? qd[c].v[e] : 0.0f;
+                sum_g += in ? g[c][e] : 0.0f;
+                sum_gh += in ? g[c][e] * hat[c][e] : 0.0f;
+                dw[c][e] += in ? dy * hat[c][e] : 0.0f;
+                db[c][e] += in ? dy : 0.0f;
+            }
+        }
+        if (Team::kAhead && row + step < p.rows) fetch(row + step);
+        sum_g = lanes_sum<G>(sum_g);
+        sum_gh = lanes_sum<G>(sum_gh);
+        if constexpr (W > 1) {
+            if ((threadIdx.x & 63) == 0) {
+                slots[parity][0][threadIdx.x >> 6] = sum_g;
+                slots[parity][1][threadIdx.x >> 6] = sum_gh;
+            }
+            __syncthreads();
+            sum_g = sum_gh = 0.0f;
+#pragma unroll
+            for (int v = 0; v < W; ++v) { sum_g += slots[parity][0][v]; sum_gh += slots[parity][1][v]; }
+        }
+        sum_g *= scale;
+        sum_gh *= scale;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const Columns<E> at(c * Team::kLanes + member, dim);
+            if constexpr (!Team::kAhead) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) d[c][e] = 0.0f;
+                if constexpr (RES)
+                    if (p.dsum) get<float, E>(p.dsum + row * dim + at.col, d[c]);
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[c][e] += rs * (g[c][e] - sum_g - hat[c][e] * sum_gh);
+            if (!RES || p.dx) put<T, E>(static_cast<T*>(p.dx) + row * dim + at.col, d[c]);
+            if constexpr (RES)
+                if (p.dresidual) put<float, E>(p.dresidual + row * dim + at.col, d[c]);
+        }
+    }
+
+    // the block's share of dweight and dbias: its teams' sums, added in a fixed order
+    float* part_w = p.part + (long)blockIdx.x * 2 * dim;
+    float* part_b = part_w + dim;
+    if constexpr (W == 1 && G == 64) {
+        if (team > 0) {
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    fold[(((team - 1) * NV + c) * 2 * E + e) * 64 + member] = dw[c][e];
+                    fold[(((team - 1) * NV + c) * 2 * E + E + e) * 64 + member] = db[c][e];
+                }
+        }
+        __syncthreads();
+        if (team > 0) return;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+#pragma unroll 1
+                for (int t = 0; t < 3; ++t) {
+                    dw[c][e] += fold[((t * NV + c) * 2 * E + e) * 64 + member];
+                    db[c][e] += fold[((t * NV + c) * 2 * E + E + e) * 64 + member];
+                }
+    } else if constexpr (G == 16) {
+        __shared__ float small[16 * 16 * NV * E * 2];
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                small[((c * 2 * E + e) * 16 + team) * 16 + member] = dw[c][e];
+                small[((c * 2 * E + E + e) * 16 + team) * 16 + member] = db[c][e];
+            }
+        __syncthreads();
+        if (team > 0) return;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+#pragma unroll 1
+                for (int t = 1; t < 16; ++t) {
+                    dw[c][e] += small[((c * 2 * E + e) * 16 + t) * 16 + member];
+                    db[c][e] += small[((c * 2 * E + E + e) * 16 + t) * 16 + member];
+                }
+    }
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const Columns<E> at(c * Team::kLanes + member, dim);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (whole || at.in(e, dim)) {
+                part_w[at.col + e] = dw[c][e];
+                part_b[at.col + e] = db[c][e];
+            }
+    }
+}
+
+// Rows too long for registers: a block a row, which reads it once for each of mean, deviation and result.
+template <typename T, bool RES>
+__global__ __launch_bounds__(1024) void norm_long_fwd_kernel(const NormParams p)
+{
+    __shared__ float slots[2][16];
+    const long at = (long)blockIdx.x * p.dim;
+    const T* x = static_cast<const T*>(p.x) + at;
+    auto value = [&](int c) { return RES ? to_f32(x[c]) + p.residual[at + c] : to_f32(x[c]); };
+    float sum = 0.0f;
+    for (int c = threadIdx.x; c < p.dim; c += 1024) {
+        const float s = value(c);
+        if constexpr (RES) p.sum[at + c] = s;
+        sum += s;
+    }
+    const float mean = team_sum<64, 16>(sum, &slots[0]) / (float)p.dim;
+    float square = 0.0f;
+    for (int c = threadIdx.x; c < p.dim; c += 1024) {
+        const float s = (RES ? p.sum[at + c] : value(c)) - mean;
+        square += s * s;
+    }
+    const float rstd = 1.0f / sqrtf(team_sum<64, 16>(square, &slots[1]) / (float)p.dim + p.eps);
+    if (p.mean && threadIdx.x == 0) { p.mean[blockIdx.x] = mean; p.rstd[blockIdx.x] = rstd; }
+    for (int c = threadIdx.x; c < p.dim; c += 1024) {
+        const float s = (RES ? p.sum[at + c] : value(c)) - mean;
+        static_cast<T*>(p.y)[at + c] = from_f32<T>(fmaf(s * rstd, p.weight ? p.weight[c] : 1.0f, p.bias ? p.bias[c] : 0.0f));
+    }
+}
+template <typename T, bool RES>
+__global__ __launch_bounds__(1024) void norm_long_bwd_kernel(const NormParams p)
+{
+    using S = std::conditional_t<RES, float, T>;
+    __shared__ float slots[2][16];
+    const long at = (long)blockIdx.x * p.dim;
+    const S* s = (RES ? reinterpret_cast<const S*>(p.sum) : static_cast<const S*>(p.x)) + at;
+    const T* dy = static_cast<const T*>(p.dy) + at;
+    const float mean = p.mean[blockIdx.x], rstd = p.rstd[blockIdx.x];
+    float sum_g = 0.0f, sum_gh = 0.0f;
+    for (int c = threadIdx.x; c < p.dim; c += 1024) {
+        const float g = to_f32(dy[c]) * (p.weight ? p.weight[c] : 1.0f);
+        sum_g += g;
+        sum_gh += g * (to_f32(s[c]) - mean) * rstd;
+    }
+    sum_g = team_sum<64, 16>(sum_g, &slots[0]) / (float)p.dim;
+    sum_gh = team_sum<64, 16>(sum_gh, &slots[1]) / (float)p.dim;
+    for (int c = threadIdx.x; c < p.dim; c += 1024) {
+        const float g = to_f32(dy[c]) * (p.weight ? p.weight[c] : 1.0f);
+        float d = rstd * (g - sum_g - (to_f32(s[c]) - mean) * rstd * sum_gh);
+        if (RES && p.dsum) d += p.dsum[at + c];
+        if (p.dx) static_cast<T*>(p.dx)[at + c] = from_f32<T>(d);
+        if (RES && p.dresidual) p.dresidual[at + c] = d;
+    }
+}
+// Their shares of dweight and dbias: a thread a column, a block's rows.
+template <typename T, bool RES>
+__global__ __launch_bounds__(256) void norm_long_columns_kernel(const NormParams p)
+{
+    using S = std::conditional_t<RES, float, T>;
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= p.dim) return;
+    const S* s = RES ? reinterpret_cast<const S*>(p.sum) : static_cast<const S*>(p.x);
+    float dw = 0.0f, db = 0.0f;
+    for (long r = blockIdx.y; r < p.rows; r += gridDim.y) {
+        const float dy = to_f32(static_cast<const T*>(p.dy)[r * p.dim + c]);
+        dw += dy * (to_f32(s[r * p.dim + c]) - p.mean[r]) * p.rstd[r];
+        db += dy;
+    }
+    p.part[(long)blockIdx.y * 2 * p.dim + c] = dw;
+    p.part[((long)blockIdx.y * 2 + 1) * p.dim + c] = db;
+}
+
+// Adds the shares of the blocks, in a fixed order: 16 columns a block, 16 threads to a column.
+__global__ __launch_bounds__(256) void norm_reduce_kernel(const float* __restrict__ part, float* __restrict__ dweight,
+                                                          float* __restrict__ dbias, int dim, int shares)
+{
+    __shared__ float sums[16][17];
+    const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
+    const long col = (long)blockIdx.x * 16 + lane, width = 2 * (long)dim;
+    float s = 0.0f;
+    if (col < width)
+        for (int k = group; k < shares; k += 16) s += part[k * width + col];
+    sums[group][lane] = s;
+    __syncthreads();
+    if (group || col >= width) return;
+    for (int g = 1; g < 16; ++g) s += sums[g][lane];
+    if (col < dim) { if (dweight) dweight[col] = s; }
+    else if (dbias) dbias[col - dim] = s;
+}
+
+// ---- launch shapes ---------------------------------------------------------------------------------
+// Elements of a pack: 16 bytes of the widest tensor of the row; rows of fewer elements go one by one.
+template <typename T, bool RES> constexpr int kPack = RES || sizeof(T) == 4 ? 4 : 8;
+
+struct NormShape { int pack, lanes, waves, packs; };              // packs == 0: the long kernels
+NormShape norm_shape(const NormParams& p)
+{
+    const int full = p.with_residual || p.dtype == 0 ? 4 : 8;
+    NormShape s{p.dim < full ? 1 : full, 64, 1, 1};
+    const int n = (p.dim + s.pack - 1) / s.pack;
+    if (n <= 16) { s.lanes = 16; return s; }
+    // at most 16 elements a lane, 24 in the widest teams
+    const int most = 16 / s.pack;
+    for (s.waves = 1; s.waves <= 8; s.waves *= 2) {
+        s.packs = (n + 64 * s.waves - 1) / (64 * s.waves);
+        if (s.packs <= most) return s;
+    }
+    s.waves = 8;
+    if (s.packs <= most * 3 / 2) { s.packs = most * 3 / 2; return s; }
+    s.packs = 0;
+    return s;
+}
+// Teams of a block.
+int norm_block_rows(const NormShape& s) { return s.packs == 0 || s.waves > 1 ? 1 : 4 * (64 / s.lanes); }
+
+template <typename T, bool RES, int E, int G, int W, int NV>
+hipError_t launch_shape(const NormParams& p, bool backward, unsigned blocks, hipStream_t stream)
+{
+    if (backward) norm_bwd_kernel<T, RES, E, G, W, NV><<<blocks, W == 1 ? 256 : 64 * W, 0, stream>>>(p);
+    else norm_fwd_kernel<T, RES, E, G, W, NV><<<blocks, W == 1 ? 256 : 64 * W, 0, stream>>>(p);
+    return hipGetLastError();
+}
+template <typename T, bool RES, int W>
+hipError_t launch_packs(const NormParams& p, int packs, bool backward, unsigned blocks, hipStream_t stream)
+{
+    constexpr int E = kPack<T, RES>, kMost = 16 / E;
+    if (packs == kMost) return launch_shape<T, RES, E, 64, W, kMost>(p, backward, blocks, stream);
+    // (several waves: the row was too long for half of them, so more than half of their packs are needed)
+    if constexpr (kMost == 4) if (packs == 3) return launch_shape<T, RES, E, 64, W, 3>(p, backward, blocks, stream);
+    if constexpr (W == 1) {
+        if (packs == 1) return launch_shape<T, RES, E, 64, W, 1>(p, backward, blocks, stream);
+        if constexpr (kMost == 4) if (packs == 2) return launch_shape<T, RES, E, 64, W, 2>(p, backward, blocks, stream);
+    }
+    if constexpr (W == 8)
+        if (packs == kMost * 3 / 2) return launch_shape<T, RES, E, 64, W, kMost * 3 / 2>(p, backward, blocks, stream);
+    return hipErrorInvalidValue;
+}
+template <typename T, bool RES>
+hipError_t launch_typed(const NormParams& p, bool backward, hipStream_t stream)
+{
+    const NormShape s = norm_shape(p);
+    if (s.packs == 0) {
+        if (p.rows > 0x7fffffffL) return hipErrorInvalidValue;
+        if (!backward) {
+            norm_long_fwd_kernel<T, RES><<<(unsigned)p.rows, 1024, 0, stream>>>(p);
+        } else {
+            norm_long_bwd_kernel<T, RES><<<(unsigned)p.rows, 1024, 0, stream>>>(p);
+            if (p.dweight || p.dbias) norm_long_columns_kernel<T, RES><<<dim3((p.dim + 255) / 256, p.shares), 256, 0, stream>>>(p);
+        }
+        return hipGetLastError();
+    }
+    const int per = norm_block_rows(s);
+    const long whole = (p.rows + per - 1) / per;
+    const unsigned blocks = backward ? p.shares : (unsigned)(whole < 2048 ? whole : 2048);
+    if (s.lanes == 16)
+        return s.pack == 1 ? launch_shape<T, RES, 1, 16, 1, 1>(p, backward, blocks, stream)
+                           : launch_shape<T, RES, kPack<T, RES>, 16, 1, 1>(p, backward, blocks, stream);
+    if (s.waves == 1) return launch_packs<T, RES, 1>(p, s.packs, backward, blocks, stream);
+    if (s.waves == 2) return launch_packs<T, RES, 2>(p, s.packs, backward, blocks, stream);
+    if (s.waves == 4) return launch_packs<T, RES, 4>(p, s.packs, backward, blocks, stream);
+    return launch_packs<T, RES, 8>(p, s.packs, backward, blocks, stream);
+}
+hipError_t launch(const NormParams& p, bool backward, hipStream_t stream)
+{
+    if (p.dtype == 0)
+        return p.with_residual ? launch_typed<float, true>(p, backward, stream) : launch_typed<float, false>(p, backward, stream);
+    return p.with_residual ? launch_typed<bf16_t, true>(p, backward, stream) : launch_typed<bf16_t, false>(p, backward, stream);
+}
+// Blocks of the backward kernel, each with a share of dweight and dbias.
+int norm_shares(const NormParams& p)
+{
+    const NormShape s = norm_shape(p);
+    const int per = norm_block_rows(s);
+    const long whole = (p.rows + per - 1) / per;
+    const long most = s.waves >= 8 || s.packs == 0 ? 256 : 512;
+    return (int)(whole < most ? whole : most);
+}
+
+}  // namespace
+
+size_t norm_bwd_floats(const NormParams& p) { return p.rows > 0 ? (size_t)norm_shares(p) * 2 * p.dim : 0; }
+
+hipError_t launch_norm_fwd(const NormParams& p, hipStream_t stream) { return launch(p, false, stream); }
+
+hipError_t launch_norm_bwd(NormParams p, float* workspace, hipStream_t stream)
+{
+    p.part = workspace;
+    p.shares = norm_shares(p);
+    hipError_t e = launch(p, true, stream);
+    if (e != hipSuccess || (!p.dweight && !p.dbias)) return e;
+    norm_reduce_kernel<<<(unsigned)((2 * (long)p.dim + 15) / 16), 256, 0, stream>>>(workspace, p.dweight, p.dbias, p.dim, p.shares);
+    return hipGetLastError();
+}
+
+}  // namespace lbscan
