@@ -78,95 +78,24 @@ def causal_conv1d_silu(x, weight, bias=None, *, activation=True, reverse=False):
     return _Conv1dSiLU.apply(x, weight, bias, bool(activation), bool(reverse))
 
 
-class _GatedRecurrence(torch.autograd.Function):
-    """y = lbscan_gated_fwd(...); gradients from lbscan_gated_bwd, which starts from the states that the forward
-    call leaves in the saved_state buffer."""
-
-    @staticmethod
-    def forward(ctx, x, gate_a, gate_x, decay, starts, h0, rate, reverse, return_state):
-        x, gate_a, gate_x = x.contiguous(), gate_a.contiguous(), gate_x.contiguous()
-        starts = None if starts is None else starts.contiguous()
-        h0 = None if h0 is None else h0.contiguous()
-        saved = sequence.lbscan_gated_saved_state(x, reverse=reverse) if any(ctx.needs_input_grad) else None
-        res = sequence.lbscan_gated_fwd(x, gate_a, gate_x, decay, rate=rate, starts=starts, reverse=reverse, h0=h0,
-                                        return_state=return_state, saved_state=saved)
-        ctx.save_for_backward(x, gate_a, gate_x, decay, starts, h0, saved)
-        ctx.cfg = (rate, reverse)
-        ctx.set_materialize_grads(False)
-        return res
-
-    @staticmethod
-    def backward(ctx, dout, dhT=None):
-        x, gate_a, gate_x, decay, starts, h0, saved = ctx.saved_tensors
-        rate, reverse = ctx.cfg
-        if dout is None and dhT is None:
-            return (None,) * 9
-        dout = torch.zeros_like(x) if dout is None else dout.contiguous()
-        g = sequence.lbscan_gated_bwd(x, gate_a, gate_x, decay, dout=dout, rate=rate, starts=starts, reverse=reverse,
-                                      h0=h0, dhT=None if dhT is None else dhT.contiguous(), saved_state=saved)
-        dh0 = g["dh0"] if h0 is not None else None
-        return g["dx"], g["dgate_a"], g["dgate_x"], g["ddecay"], None, dh0, None, None, None
-
+# The operators around the scan.  Their autograd nodes are in csrc/lbscan_torch.cpp: these calls are short, and
+# a node in Python costs more host time than their kernels take.
 
 def gated_linear_recurrence(x, gate_a, gate_x, decay, *, rate=8.0, starts=None, reverse=False, h0=None,
                             return_state=False):
     """Differentiable gated linear recurrence along the last axis of x, gate_a, gate_x (B,D,L), with decay (D)
     and h0 (B,D) fp32, starts (B,L) bool or uint8 (see include/lbscan.h).  Returns y, or (y, hT) with
     return_state."""
-    return _GatedRecurrence.apply(x, gate_a, gate_x, decay, starts, h0, float(rate), bool(reverse),
-                                  bool(return_state))
-
-
-class _LayerNorm(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x, weight, bias, residual, eps):
-        x = x.contiguous()
-        residual = None if residual is None else residual.contiguous()
-        res = sequence.lbscan_norm_fwd(x, weight, bias, residual=residual, eps=eps, return_stats=True)
-        mean, rstd = res[-2:]
-        total = None if residual is None else res[1]
-        # (with a residual x is not read again)
-        ctx.save_for_backward(x if total is None else None, weight, mean, rstd, total)
-        ctx.cfg = (bias is not None, x.dtype)
-        ctx.set_materialize_grads(False)
-        return res[0] if total is None else res[:2]
-
-    @staticmethod
-    def backward(ctx, dout, dsum=None):
-        x, weight, mean, rstd, total = ctx.saved_tensors
-        with_bias, dtype = ctx.cfg
-        if dout is None and dsum is None:
-            return (None,) * 5
-        if dout is None:
-            dout = torch.zeros_like(total if x is None else x, dtype=dtype)
-        dout = dout.contiguous()
-        g = sequence.lbscan_norm_bwd(x, weight, dout=dout, mean=mean, rstd=rstd, with_bias=with_bias, total=total,
-                                     dsum=None if dsum is None else dsum.contiguous())
-        return g["dx"], g["dweight"], g["dbias"], g["dresidual"], None
+    return sequence.load().gated(x, gate_a, gate_x, decay, starts, h0, rate, reverse, return_state)
 
 
 def layer_norm(x, weight=None, bias=None, *, residual=None, eps=1e-5):
     """Differentiable layer norm over the last axis of x; weight, bias (dim) fp32.  With residual (fp32,
     x's shape) x + residual is normalised and (y, x + residual) returned, the sum in fp32."""
-    return _LayerNorm.apply(x, weight, bias, residual, float(eps))
-
-
-class _TokenEmbedding(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, ids, weight, scale):
-        ids, weight = ids.contiguous(), weight.contiguous()
-        ctx.save_for_backward(ids)
-        ctx.cfg = (scale, weight.shape[0])
-        return sequence.lbscan_embed_fwd(ids, weight, scale=scale)
-
-    @staticmethod
-    def backward(ctx, dout):
-        ids, = ctx.saved_tensors
-        scale, vocab = ctx.cfg
-        return None, sequence.lbscan_embed_bwd(ids, dout=dout.contiguous(), vocab=vocab, scale=scale), None
+    return sequence.load().norm(x, weight, bias, residual, eps)
 
 
 def token_embedding(ids, weight, *, scale=1.0):
     """Differentiable scale * weight[ids]: ids int32 or int64 of any shape, weight (vocab, dim); zeros (and no
     gradient) for ids that are no row of the table."""
-    return _TokenEmbedding.apply(ids, weight, float(scale))
+    return sequence.load().embed(ids, weight, scale)

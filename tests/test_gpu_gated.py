@@ -223,14 +223,16 @@ def test_steps_equal_the_prompt(lb, dtype):
 def test_state_in_place(lb, B, D, L):
     """hT may be h0, also where a row is cut and every piece reads the state that enters."""
     import ctypes
-    from paper_2506_15976_amd import binding, sequence
+    from paper_2506_15976_amd import binding
     t, _ = make(B, D, L, seed=12)
     y, hT = lb.lbscan_gated_fwd(**t, return_state=True)
     state, out = t["h0"].clone(), torch.empty_like(t["x"])
-    a = sequence._gated_args(t["x"], t["gate_a"], t["gate_x"], t["decay"], None, state, out, state, 8.0, False, None)
-    ws = sequence._gated_scratch(a, binding.WS_FWD, t["x"], None)
+    a = lb.LbscanGatedArgs(B, D, L, 0, 0, 8.0, t["x"].data_ptr(), t["gate_a"].data_ptr(), t["gate_x"].data_ptr(),
+                           t["decay"].data_ptr(), None, state.data_ptr(), out.data_ptr(), state.data_ptr())
+    a.workspace_bytes = lb.load().lbscan_gated_workspace_bytes(ctypes.byref(a), binding.WS_FWD)
+    ws = torch.empty(a.workspace_bytes + 4, dtype=torch.uint8, device="cuda")
+    a.workspace = ws.data_ptr()
     assert lb.load().lbscan_gated_fwd(ctypes.byref(a), binding._stream(None)) == 0
-    del ws
     assert torch.equal(out, y) and torch.equal(state, hT)
 
 

@@ -139,9 +139,10 @@ def test_alignment_and_in_place(lb, dim, dtype):
     assert all(torch.equal(a[k], b[k]) for k in a)
     # y over x, and through the C entry the sum over the residual
     import ctypes
-    from paper_2506_15976_amd import binding, sequence
+    from paper_2506_15976_amd import binding
     x, r = t["x"].clone(), t["residual"].clone()
-    args = sequence._norm_args(x, t["weight"], t["bias"], r, x, r, None, None, 1e-5)
+    args = lb.LbscanNormArgs(7, dim, int(dtype == "bf16"), 1e-5, x.data_ptr(), r.data_ptr(), t["weight"].data_ptr(),
+                             t["bias"].data_ptr(), x.data_ptr(), r.data_ptr())
     assert lb.load().lbscan_norm_fwd(ctypes.byref(args), binding._stream(None)) == 0
     assert torch.equal(x, y) and torch.equal(r, s)
 

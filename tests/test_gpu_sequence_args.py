@@ -1,0 +1,72 @@
+"""What the torch side of the operators around the scan refuses on the device."""
+import pytest
+import torch
+
+from paper_2506_15976_amd.binding import EINVAL, EUNSUPPORTED, LbscanError
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lb():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2506_15976_amd as pkg
+    pkg.load()
+    return pkg
+
+
+def refused(code, f, *args, **k):
+    with pytest.raises(LbscanError) as e:
+        f(*args, **k)
+    assert e.value.code == code
+
+
+def t(*shape, dtype=torch.float32):
+    return torch.zeros(*shape, dtype=dtype, device="cuda")
+
+
+def test_gated(lb):
+    from paper_2506_15976_amd.autograd import gated_linear_recurrence
+    row = t(2, 3, 8)
+    good = dict(x=row, gate_a=row, gate_x=row, decay=t(3))
+    for bad in (dict(gate_a=t(2, 3, 7)), dict(gate_x=t(2, 3, 8, dtype=torch.bfloat16)), dict(decay=t(2)), dict(decay=t(3).cpu()),
+                dict(h0=t(2, 4)), dict(h0=t(2, 3, dtype=torch.bfloat16)), dict(starts=t(2, 7, dtype=torch.bool)),
+                dict(out=t(2, 8, 3).transpose(1, 2)), dict(x=t(2, 8, 3).transpose(1, 2)), dict(decay=t(3, dtype=torch.bfloat16)),
+                dict(rate=-1.0), dict(rate=float("nan"))):
+        refused(EINVAL, lb.lbscan_gated_fwd, **{**good, **bad})
+        if "out" not in bad:
+            refused(EINVAL, lb.lbscan_gated_bwd, **{**good, **bad}, dout=row)
+    refused(EUNSUPPORTED, lb.lbscan_gated_fwd, **good, starts=t(2, 8, dtype=torch.int64))
+    for dout in (t(2, 3, 7), t(2, 3, 8, dtype=torch.bfloat16), row.cpu()):
+        refused(EINVAL, lb.lbscan_gated_bwd, **good, dout=dout)
+    refused(EINVAL, lb.lbscan_gated_bwd, **good, dout=row, dhT=t(2, 4))
+    refused(EINVAL, gated_linear_recurrence, **{**good, "decay": t(4)})
+    long = t(64, 256, 3000)
+    few = t(8)
+    refused(-3, lb.lbscan_gated_fwd, long, long, long, t(256), saved_state=few)
+    one = t(2, 3)
+    refused(EINVAL, lb.lbscan_gated_step, one, one, one, t(3), t(2, 4))
+    refused(EINVAL, lb.lbscan_gated_step, one, one, one, t(3), one.t().contiguous().t())
+    refused(EINVAL, lb.lbscan_gated_step, one, one, one, t(3), one, starts=t(3, dtype=torch.bool))
+
+
+def test_norm(lb):
+    x, w, m = t(4, 16), t(16), t(4)
+    for bad in (dict(weight=t(15)), dict(bias=t(16, dtype=torch.bfloat16)), dict(residual=t(4, 15)),
+                dict(residual=t(4, 16, dtype=torch.bfloat16)), dict(out=t(16, 4).t()), dict(eps=-1.0), dict(weight=w.cpu())):
+        refused(EINVAL, lb.lbscan_norm_fwd, x, **bad)
+    refused(EINVAL, lb.lbscan_norm_fwd, t(16, 4).t())
+    good = dict(dout=x, mean=m, rstd=m)
+    for bad in (dict(dout=t(4, 15)), dict(mean=t(5)), dict(rstd=m.double()), dict(total=t(4, 15)), dict(total=x, dsum=t(3, 16))):
+        refused(EINVAL, lb.lbscan_norm_bwd, x, w, **{**good, **bad})
+
+
+def test_embed(lb):
+    ids, table = t(7, dtype=torch.int64), t(5, 8)
+    refused(EINVAL, lb.lbscan_embed_fwd, ids, t(8, 5).t())
+    refused(EINVAL, lb.lbscan_embed_fwd, ids, table, out=t(6, 8))
+    refused(EINVAL, lb.lbscan_embed_fwd, ids.cpu(), table)
+    refused(EINVAL, lb.lbscan_embed_fwd, ids, table[:0])
+    refused(EUNSUPPORTED, lb.lbscan_embed_fwd, t(7, dtype=torch.int16), table)
+    refused(EINVAL, lb.lbscan_embed_bwd, ids, dout=t(8, 7).t(), vocab=5)
+    refused(EINVAL, lb.lbscan_embed_bwd, ids, dout=t(7, 8), vocab=0)

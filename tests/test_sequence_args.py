@@ -5,40 +5,17 @@ import pytest
 import torch
 
 from paper_2506_15976_amd import binding, sequence
+from paper_2506_15976_amd.autograd import gated_linear_recurrence, layer_norm, token_embedding
 from paper_2506_15976_amd.binding import EINVAL, EUNSUPPORTED, EWORKSPACE, OK, LbscanError
 
 
 @pytest.fixture(scope="module")
 def lib():
     import os
-    if not os.path.exists(binding.LIB_PATH):
+    if not (os.path.exists(binding.LIB_PATH) and os.path.exists(sequence.TORCH_LIB_PATH)):
         from paper_2506_15976_amd import build
         build.build(force=True, verbose=False)
     return binding.load()
-
-
-class DeviceTensor:
-    """Shape, type and address of a device tensor; nothing reads it."""
-    is_cuda = True
-
-    def __init__(self, *shape, dtype=torch.float32, contiguous=True):
-        self.shape, self.dtype, self.contiguous, self.device = torch.Size(shape), dtype, contiguous, "cuda"
-
-    def is_contiguous(self):
-        return self.contiguous
-
-    def data_ptr(self):
-        return 4096
-
-    def dim(self):
-        return len(self.shape)
-
-    def numel(self):
-        return self.shape.numel()
-
-
-class Stream:
-    cuda_stream = 0
 
 
 P = 4096                                          # an address that is never read
@@ -166,46 +143,51 @@ def test_embed_backward_refuses(lib):
     assert lib.lbscan_embed_workspace_bytes(embed(tokens=1000)) > lib.lbscan_embed_workspace_bytes(embed()) > 0
 
 
-def refused(code, f, *args, **k):
+# ---- the torch side: shapes and types are looked at before the device ------------------------------
+
+def refused(code, f, *args, says="", **k):
     with pytest.raises(LbscanError) as e:
-        f(*args, stream=Stream(), **k)
-    assert e.value.code == code
+        f(*args, **k)
+    assert e.value.code == code and says in str(e.value), str(e.value)
+
+
+def t(*shape, dtype=torch.float32):
+    return torch.zeros(*shape, dtype=dtype)
+
+
+def test_tensors_not_on_the_device():
+    row, decay = t(2, 3, 8), t(3)
+    refused(EINVAL, sequence.lbscan_gated_fwd, row, row, row, decay, says="device tensor")
+    refused(EINVAL, sequence.lbscan_gated_step, row[..., 0], row[..., 0], row[..., 0], decay, t(2, 3), says="device tensor")
+    refused(EINVAL, sequence.lbscan_norm_fwd, row, says="device tensor")
+    refused(EINVAL, sequence.lbscan_embed_fwd, t(4, dtype=torch.int64), t(5, 8), says="device tensor")
+    refused(EINVAL, gated_linear_recurrence, row, row, row, decay, says="device tensor")
+    refused(EINVAL, layer_norm, row, says="device tensor")
+    refused(EINVAL, token_embedding, t(4, dtype=torch.int64), t(5, 8), says="device tensor")
 
 
 def test_gated_binding_refuses():
-    row, decay = DeviceTensor(2, 3, 8), DeviceTensor(3)
-    good = dict(x=row, gate_a=row, gate_x=row, decay=decay, out=row)
-    for bad in (dict(gate_a=DeviceTensor(2, 3, 7)), dict(gate_x=DeviceTensor(2, 3, 8, dtype=torch.bfloat16)),
-                dict(decay=DeviceTensor(2)), dict(decay=None), dict(gate_a=None), dict(h0=DeviceTensor(2, 4)),
-                dict(starts=DeviceTensor(2, 7, dtype=torch.bool)), dict(out=DeviceTensor(2, 3, 8, contiguous=False)),
-                dict(decay=DeviceTensor(3, dtype=torch.bfloat16))):
-        refused(EINVAL, sequence.lbscan_gated_fwd, **{**good, **bad})
-    refused(EUNSUPPORTED, sequence.lbscan_gated_fwd, **{**good, "starts": DeviceTensor(2, 8, dtype=torch.int64)})
-    half = DeviceTensor(2, 3, 8, dtype=torch.float16)
-    refused(EUNSUPPORTED, sequence.lbscan_gated_fwd, half, half, half, decay, out=half)
-    one = DeviceTensor(2, 3)
-    refused(EINVAL, sequence.lbscan_gated_step, one, one, one, decay, None, out=one)
-    refused(EINVAL, sequence.lbscan_gated_step, one, one, one, decay, DeviceTensor(2, 4), out=one)
-    refused(EINVAL, sequence.lbscan_gated_step, row, row, row, decay, one, out=row)
+    row = t(2, 3, 8)
+    refused(EINVAL, sequence.lbscan_gated_fwd, t(2, 3), t(2, 3), t(2, 3), t(3), says="3 axes")
+    half = t(2, 3, 8, dtype=torch.float16)
+    refused(EUNSUPPORTED, sequence.lbscan_gated_fwd, half, half, half, t(3), says="dtype")
+    refused(EINVAL, sequence.lbscan_gated_step, row, row, row, t(3), t(2, 3), says="2 axes")
+    with pytest.raises(TypeError):
+        sequence.lbscan_gated_step(row, row, row, t(3), None)
 
 
 def test_norm_binding_refuses():
-    x, w = DeviceTensor(4, 16), DeviceTensor(16)
-    refused(EINVAL, sequence.lbscan_norm_fwd, x, DeviceTensor(15), w, out=x)
-    refused(EINVAL, sequence.lbscan_norm_fwd, x, w, DeviceTensor(16, dtype=torch.bfloat16), out=x)
-    refused(EINVAL, sequence.lbscan_norm_fwd, x, w, w, out=DeviceTensor(4, 16, contiguous=False))
-    refused(EUNSUPPORTED, sequence.lbscan_norm_fwd, DeviceTensor(4, 16, dtype=torch.float16), w, w,
-            out=DeviceTensor(4, 16, dtype=torch.float16))
-    m = DeviceTensor(4)
-    refused(EINVAL, sequence.lbscan_norm_bwd, x, w, dout=x, mean=None, rstd=m)
-    refused(EINVAL, sequence.lbscan_norm_bwd, None, w, dout=x, mean=m, rstd=m)
-    refused(EINVAL, sequence.lbscan_norm_bwd, x, w, dout=x, mean=m, rstd=m, dsum=x)
+    x, m = t(4, 16), t(4)
+    refused(EUNSUPPORTED, sequence.lbscan_norm_fwd, t(4, 16, dtype=torch.float16), says="dtype")
+    refused(EINVAL, sequence.lbscan_norm_fwd, t(()), says="axis")
+    refused(EINVAL, sequence.lbscan_norm_bwd, None, dout=x, mean=m, rstd=m, says="required")
+    refused(EINVAL, sequence.lbscan_norm_bwd, x, dout=x, mean=m, rstd=m, dsum=x, says="dsum")
 
 
 def test_embed_binding_refuses():
-    ids, table = DeviceTensor(7, dtype=torch.int64), DeviceTensor(5, 8)
-    refused(EUNSUPPORTED, sequence.lbscan_embed_fwd, DeviceTensor(7, dtype=torch.float32), table, out=DeviceTensor(7, 8))
-    refused(EINVAL, sequence.lbscan_embed_fwd, ids, DeviceTensor(5, 8, 2), out=DeviceTensor(7, 8))
-    refused(EINVAL, sequence.lbscan_embed_fwd, ids, table, out=DeviceTensor(6, 8))
-    refused(EINVAL, sequence.lbscan_embed_fwd, ids, DeviceTensor(5, 8, contiguous=False), out=DeviceTensor(7, 8))
-    refused(EINVAL, sequence.lbscan_embed_bwd, ids, dout=DeviceTensor(6, 8), vocab=5)
+    ids = t(7, dtype=torch.int64)
+    refused(EUNSUPPORTED, sequence.lbscan_embed_fwd, t(7), t(5, 8), says="int32 or int64")
+    refused(EINVAL, sequence.lbscan_embed_fwd, ids, t(5, 8, 2), says="2 axes")
+    refused(EINVAL, sequence.lbscan_embed_bwd, ids, dout=t(6, 8), vocab=5, says="shape of ids")
+    refused(EINVAL, sequence.lbscan_embed_bwd, ids, dout=t(7), vocab=5, says="shape of ids")
+    refused(EINVAL, sequence.lbscan_embed_bwd, ids, dout=t(7, 8), vocab=-1, says="vocab")
