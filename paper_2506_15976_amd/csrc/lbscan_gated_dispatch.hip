@@ -6,29 +6,58 @@ namespace lbscan {
 namespace {
 
 // ddecay[d] = sigma(decay) / softplus(decay) * sum over batch entries and segments of the rows' sums, in a
-// fixed order.  64 channels a block, four threads to a channel.
+// fixed order.  16 channels a block, 16 threads to a channel.
 __global__ __launch_bounds__(256) void gated_decay_kernel(const float* __restrict__ qsum, const float* __restrict__ decay,
                                                           float* __restrict__ ddecay, int dim, int shares)
 {
-    __shared__ float part[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
+    __shared__ float part[16][17];
+    const int lane = threadIdx.x & 15, group = threadIdx.x >> 4, d = blockIdx.x * 16 + lane;
     float s = 0.0f;
-    if (d < dim)
-        for (int k = wave; k < shares; k += 4) s += qsum[(long)k * dim + d];
-    part[wave][lane] = s;
+    if (d < dim) {
+#pragma unroll 4
+        for (int k = group; k < shares; k += 16) s += qsum[(long)k * dim + d];
+    }
+    part[group][lane] = s;
     __syncthreads();
-    if (wave || d >= dim) return;
+    if (group || d >= dim) return;
+#pragma unroll
+    for (int g = 1; g < 16; ++g) s += part[g][lane];
     float slope;
     const float soft = softplus_f32(decay[d], slope);
     // (both go with e^decay where it is small, down to where they underflow)
-    const float ratio = decay[d] < -16.0f ? 1.0f : slope / soft;
-    ddecay[d] = ((part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane])) * ratio;
+    ddecay[d] = s * (decay[d] < -16.0f ? 1.0f : slope / soft);
 }
 
 hipError_t launch_kernels(const GatedParams& p, GatedPass pass, hipStream_t stream)
 {
     if (p.dtype == 0) return p.reverse ? launch_gated_f32_rev(p, pass, stream) : launch_gated_f32(p, pass, stream);
     return p.reverse ? launch_gated_bf16_rev(p, pass, stream) : launch_gated_bf16(p, pass, stream);
+}
+
+// Waves of a row's team, for a row of so many wave tiles (the tokens of 64 lanes).  As few idle lanes as possible
+// first: a tile that the row does not fill costs as much as a full one.  Among equals a tile that holds the
+// whole row (nothing is carried along: 81 registers instead of 115 in the backward kernel), then the order below.  Fewer
+// waves than 8 a CU do not keep the memory busy, and sixteen to a team leave room for one
+// team a CU with 2-byte storage (there they are for few rows only).  MI355X, us, forward / backward, by waves a
+// team:
+//     8 x 768 x 4096 bf16     1: 42.7 / 78.2    4: 43.4 / 76.8    8: 41.6 / 72.9    16: 68.5 / 148.8
+//     8 x 768 x 4096 fp32     1: 82.1 / 151.6   4: 78.5 / 141.4   8: 73.6 / 134.8   16: 70.9 / 131.7
+//     1 x 768 x 8192 bf16     1: 16.4 / 33.6    4: 11.7 / 22.8    8: 12.0 / 23.7    16: 11.3 / 27.4
+//     1 x 256 x 65536 fp32    1: 193.6 / 321.4  4: 59.7 / 133.0   8: 48.4 / 104.2   16: 49.5 / 97.4
+//     1 x 384 x 20000 bf16    1: 37.2 / 78.4    4: 18.4 / 33.7    8: 16.1 / 30.1    16: 19.2 / 35.8
+//     4 x 1000 x 3001 bf16    1: 21.8 / 38.3    4: 25.6 / 47.0    8: 25.0 / 47.4    16: 44.3 / 106.7
+//     16 x 512 x 700 bf16     1: 13.7 / 25.3    2: 12.7 / 25.2    4: 20.7 / 39.5
+int team_waves(int wave_tiles, long rows, int dtype)
+{
+    int best = 0, padded = 0;
+    for (const int w : {8, 4, 1, 2, 16}) {
+        if (w > 1 && w >= 2 * wave_tiles) continue;                    // half of it would idle
+        if (w < 16 && w < wave_tiles && rows * w <= 2048) continue;
+        if (w == 16 && best && dtype != 0) continue;
+        const int n = (wave_tiles + w - 1) / w * w;
+        if (!best || n < padded || (n == padded && n == w)) { best = w; padded = n; }
+    }
+    return best;
 }
 
 long rows_of_call(const GatedParams& p) { return (long)p.batch * p.dim; }
@@ -49,14 +78,14 @@ void gated_shape(GatedParams& p)
     p.lanes = 8;
     while (p.lanes < 64 && p.lanes * v < L) p.lanes *= 2;
     const int wave_tiles = (L + 64 * v - 1) / (64 * v);
-    if (wave_tiles > 2) {
-        if (rows < 4096 && wave_tiles >= 9) p.waves = 16;
-        else if (rows < 8192) p.waves = 4;
-    }
+    if (wave_tiles > 1) p.waves = team_waves(wave_tiles, rows, p.dtype);
     const int tile = p.lanes * p.waves * v;
     p.ntiles = p.seg_tiles = (L + tile - 1) / tile;
-    if (rows < 256 && p.ntiles > 1) {
-        int want = (int)((512 + rows - 1) / rows);
+    // A row is cut where there are too few for the CUs; the maps of the pieces cost another pass over three of the
+    // tensors.  MI355X, us, forward / backward, whole and cut: 1 x 64 x 65536 bf16 22.5 / 38.8 and 16.6 / 22.5,
+    // 1 x 16 x 65536 fp32 22.9 / 40.9 and 8.8 / 13.3, 1 x 128 x 65536 fp32 30.1 / 56.6 and 40.3 / 61.4.
+    if (rows <= 96 && p.ntiles > 1) {
+        int want = (int)((256 + rows - 1) / rows);
         want = want < 64 ? want : 64;                      // a lane folds a segment
         want = want < p.ntiles ? want : p.ntiles;
         p.seg_tiles = (p.ntiles + want - 1) / want;
@@ -120,7 +149,7 @@ hipError_t launch_gated_bwd(GatedParams p, float* workspace, const float* saved,
     }
     if (p.nseg > 1 && (e = launch_kernels(p, GatedPass::backward_summary, stream)) != hipSuccess) return e;
     if ((e = launch_kernels(p, GatedPass::backward, stream)) != hipSuccess) return e;
-    gated_decay_kernel<<<(p.dim + 63) / 64, 256, 0, stream>>>(p.qsum, p.decay, p.ddecay, p.dim, p.nseg * p.batch);
+    gated_decay_kernel<<<(p.dim + 15) / 16, 256, 0, stream>>>(p.qsum, p.decay, p.ddecay, p.dim, p.nseg * p.batch);
     return hipGetLastError();
 }
 

@@ -90,7 +90,7 @@ def test_gated_scratch_follows_the_plan(lib, dtype):
     assert [size(w, seqlen=100) for w in (FWD, BWD, SAVED)] == [0, 6 * 4, 0]
     assert [size(w, seqlen=3) for w in (FWD, BWD, SAVED)] == [0, 6 * 4, 0]
     # several tiles: the states at their starts, kept by the caller or computed again
-    many = dict(batch=64, dim=256, seqlen=2000)
+    many = dict(batch=64, dim=256, seqlen=60000)
     assert size(FWD, **many) == 0 and size(SAVED, **many) % (64 * 256 * 4) == 0 and size(SAVED, **many) > 0
     assert size(BWD, **many) == size(BWD, saved_state=P, **many) + size(SAVED, **many)
     # few long rows are cut
