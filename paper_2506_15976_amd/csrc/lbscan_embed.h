@@ -24,6 +24,9 @@ struct EmbedParams {
     int* row;
     int* count;               // (vocab)
     int* valid;
+    int* share_total;         // tokens of (share of the tokens, block of rows), and of each of its rows
+    int* share_count;
+    int blocks_log2, shares;  // the sort's grid
     float* part;              // (pieces, 2, dim)
 };
 

@@ -4,6 +4,8 @@
 #include "lbscan_embed.h"
 #include "lbscan_internal.h"
 
+#include <type_traits>
+
 namespace lbscan {
 namespace {
 
@@ -52,112 +54,185 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const EmbedParams p)
 }
 
 // ---- gradient: the tokens sorted by row ------------------------------------------------------------
-// One launch.  Block r of R (a power of two) has the rows v = r mod R, so that rows that are used much and lie
-// next to each other in a table ordered by frequency go to different blocks.  Every block reads all ids:
-// it counts those of blocks before it, which is where its own begin, and its own by row and by sixteenth
-// of the tokens (a wave each).  The running sums of these counts are where each wave puts its tokens; a wave
-// takes its tokens in order, so that those of a row stay in the order of the tokens.
+// A stable counting sort.  Block (r, c) has the rows v = r mod R, R a power of two (so that rows that are used much and
+// lie next to each other in a table ordered by frequency go to different blocks), and the c-th share of the
+// tokens.  It looks at every id of its share and counts those of its rows, by row and by sixteenth of the share (a
+// wave each).  Running sums of the counts over rows, shares and waves say where each wave puts its tokens; a wave takes
+// them in order, so that the tokens of a row stay in theirs.  One share: one launch, in which a block also
+// counts the tokens of the blocks before it.  Several: a launch that counts and one that places, since what
+// takes the time is one wave walking through the tokens of a much used row.  MI355X, us, Zipf's law over 50000 rows,
+// the call with one share and with eight: 32768 x 768 bf16
+// 48.3 / 43.6, 65536 x 512 bf16 over 300 rows 63.7 / 42.7.
 constexpr int kSortWaves = 16;
-constexpr int kSortRows = 512;             // most rows of a block: 32 KB of counts
-constexpr int kSortAhead = 4;              // groups of 64 ids that a wave loads together
+constexpr int kSortRows = 896;             // most rows of a block: 56 KB of counts, and a thread each
+constexpr int kSortShare = 4096;           // tokens of a share, where the grid allows
+constexpr int kSortShares = 8;             // most shares: two blocks a CU where there are 64 of rows
+constexpr int kSortAhead = 4;              // groups of 64 ids that a wave loads together at first
 
-int sort_blocks_log2(int vocab)
+enum class Sort { all, count, place };
+
+void sort_shape(EmbedParams& p)
 {
-    int log2 = 8;
-    while (((long)kSortRows << log2) < vocab) ++log2;
-    return log2;
+    p.blocks_log2 = 6;
+    while (((long)kSortRows << p.blocks_log2) < p.vocab) ++p.blocks_log2;
+    const long most = (kSortShares << 6) >> p.blocks_log2, wanted = (p.tokens + kSortShare - 1) / kSortShare;
+    p.shares = (int)(wanted < most ? wanted : most);
+    if (p.shares < 1) p.shares = 1;
+}
+int sort_rows(const EmbedParams& p) { return (int)(((unsigned)p.vocab + (1u << p.blocks_log2) - 1) >> p.blocks_log2); }
+
+// The row of an id, with the top bit set where it is none (vocab < 2^31).
+template <typename I>
+__device__ __forceinline__ unsigned sort_row(I id, unsigned vocab)
+{
+    using U = std::make_unsigned_t<I>;
+    return (U)id < (U)vocab ? (unsigned)id : 0xffffffffu;
 }
 
-template <typename I>
-__global__ __launch_bounds__(64 * kSortWaves) void embed_sort_kernel(const EmbedParams p, int blocks_log2)
+// Sum over the block's threads, the same in all of them.
+__device__ __forceinline__ int block_sum(int v, int (&totals)[kSortWaves])
 {
-    extern __shared__ int counts[];        // (waves, rows)
-    __shared__ int totals[kSortWaves];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int mine = blockIdx.x, mask = (1 << blocks_log2) - 1;
-    const int rows = (p.vocab - mine + mask) >> blocks_log2;          // v = mine + k * blocks < vocab
-    const I* ids = static_cast<const I*>(p.ids);
-    const long share = ((p.tokens + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
-    const long begin = min(share * wave, p.tokens), end = min(begin + share, p.tokens);
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) v += __shfl_xor(v, m);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) totals[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) v += totals[w];
+    return v;
+}
 
+template <typename I, Sort WHAT>
+__global__ __launch_bounds__(64 * kSortWaves) void embed_sort_kernel(const EmbedParams p)
+{
+    extern __shared__ int counts[];        // (waves, rows), and a place per lane for what does not count
+    __shared__ int totals[kSortWaves];
+    const int blocks_log2 = p.blocks_log2;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned mine = blockIdx.x, mask = (1u << blocks_log2) - 1;
+    const unsigned mask_none = mask | 0x80000000u;
+    const int rows = (int)(((unsigned)p.vocab + mask - mine) >> blocks_log2);   // v = mine + k * blocks < vocab
+    const I* ids = static_cast<const I*>(p.ids);
+    // the block's share of the tokens, and the wave's of that: whole groups of 64
+    const long block_share = ((p.tokens + gridDim.y - 1) / gridDim.y + 63) / 64 * 64;
+    const long block_begin = min(block_share * blockIdx.y, p.tokens), block_end = min(block_begin + block_share, p.tokens);
+    const long share = ((block_end - block_begin + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+    const long begin = min(block_begin + share * wave, block_end), end = min(begin + share, block_end);
+    // A bit of `hits` stands for 2^span_log2 groups of 64 ids and says whether one is the block's.
+    int span_log2 = 0;
+    while ((share >> 6 >> span_log2) > 64) ++span_log2;
+    uint64_t hits = 0;
+
+    // what the launch before left is on its way meanwhile: a thread a row; `all`: over all shares, `before`: over those
+    // before this one
+    const int row = threadIdx.x, row_pitch = ((unsigned)p.vocab + mask) >> blocks_log2;
+    int all = 0, before = 0, below = 0;
+    if constexpr (WHAT == Sort::place) {
+        const int* of_row = p.share_count + (long)mine * row_pitch + min(row, rows - 1);
+#pragma unroll
+        for (unsigned c = 0; c < kSortShares; ++c) {
+            const int v = c < gridDim.y ? of_row[(long)c * gridDim.x * row_pitch] : 0;
+            before += c < blockIdx.y ? v : 0;
+            all += v;
+        }
+        if (row >= rows) all = before = 0;
+        static_assert(kSortShares << 6 <= 64 * kSortWaves);
+        if (threadIdx.x < gridDim.x * gridDim.y) below = (threadIdx.x & mask) < mine ? p.share_total[threadIdx.x] : 0;
+    }
     for (int k = threadIdx.x; k < rows * kSortWaves; k += 64 * kSortWaves) counts[k] = 0;
     __syncthreads();
-    int below = 0;
-    for (long t = begin; t < end; t += 64 * kSortAhead) {
-        int v[kSortAhead];
+    // Every block looks at every id: whole groups are loaded without a check, and no lane waits for a branch (ids of
+    // other blocks are counted where nobody looks).
+    const int nowhere = rows * kSortWaves + lane, base = wave * rows;
+    auto count = [&](unsigned v, int group) {
+        const unsigned block = v & mask_none;
+        if (WHAT == Sort::all) below += block < mine;
+        const bool match = block == mine;
+        atomicAdd(&counts[match ? base + (int)(v >> blocks_log2) : nowhere], 1);
+        hits |= (uint64_t)(__ballot(match) != 0) << (group >> span_log2);
+    };
+    int group = 0;
+    long t = begin;
+    for (; t + 64 * kSortAhead <= end; t += 64 * kSortAhead, group += kSortAhead) {
+        const I* at = ids + t + lane;
+        I id[kSortAhead];
 #pragma unroll
-        for (int k = 0; k < kSortAhead; ++k) {
-            const long at = t + 64 * k + lane;
-            v[k] = row_of(ids[min(at, p.tokens - 1)], p.vocab);
-            if (at >= end) v[k] = -1;
-        }
+        for (int k = 0; k < kSortAhead; ++k) id[k] = at[64 * k];
 #pragma unroll
-        for (int k = 0; k < kSortAhead; ++k) {
-            below += v[k] >= 0 && (v[k] & mask) < mine;
-            if (v[k] >= 0 && (v[k] & mask) == mine) atomicAdd(&counts[wave * rows + (v[k] >> blocks_log2)], 1);
-        }
+        for (int k = 0; k < kSortAhead; ++k) count(sort_row(id[k], p.vocab), group + k);
     }
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) below += __shfl_xor(below, m);
-    if (lane == 0) totals[wave] = below;
-    __syncthreads();
-    below = 0;
-    for (int w = 0; w < kSortWaves; ++w) below += totals[w];
+    for (; t < end; t += 64, ++group) {
+        const I id = ids[min(t + lane, end - 1)];
+        count(t + lane < end ? sort_row(id, p.vocab) : 0xffffffffu, group);
+    }
     __syncthreads();
 
-    // running sums, rows first: a thread a row
+    // running sums, rows first
     int n = 0;
-    if ((int)threadIdx.x < rows) {
-        for (int w = 0; w < kSortWaves; ++w) n += counts[w * rows + threadIdx.x];
-        p.count[mine + ((int)threadIdx.x << blocks_log2)] = n;
+    if (row < rows)
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) n += counts[w * rows + row];
+    if constexpr (WHAT == Sort::count) {
+        if (row < rows) p.share_count[((long)blockIdx.y * gridDim.x + mine) * row_pitch + row] = n;
+        n = block_sum(n, totals);
+        if (threadIdx.x == 0) p.share_total[blockIdx.y * gridDim.x + mine] = n;
+        return;
     }
-    int sum = n;
+    if (WHAT == Sort::all) all = n;
+    below = block_sum(below, totals);
+    if (row < rows && blockIdx.y == 0) p.count[mine + ((unsigned)row << blocks_log2)] = all;
+    int sum = all;
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
         const int other = __shfl_up(sum, m);
         if (lane >= m) sum += other;
     }
+    __syncthreads();
     if (lane == 63) totals[wave] = sum;
     __syncthreads();
-    int at = below + sum - n, own = 0;
+    int at = below + sum - all + before, own = 0;
     for (int w = 0; w < kSortWaves; ++w) {
         if (w < wave) at += totals[w];
         own += totals[w];
     }
-    if ((int)threadIdx.x < rows)
+    if (row < rows)
         for (int w = 0; w < kSortWaves; ++w) {
-            const int c = counts[w * rows + threadIdx.x];
-            counts[w * rows + threadIdx.x] = at;
+            const int c = counts[w * rows + row];
+            counts[w * rows + row] = at;
             at += c;
         }
-    if (mine == mask && threadIdx.x == 0) *p.valid = below + own;
+    if (mine == mask && blockIdx.y == 0 && threadIdx.x == 0) *p.valid = below + own;
     __syncthreads();
 
-    volatile int* next = counts + wave * rows;       // of this wave alone
-    for (long t = begin; t < end; t += 64 * kSortAhead) {
-        int v[kSortAhead];
-#pragma unroll
-        for (int k = 0; k < kSortAhead; ++k) {
-            const long i = t + 64 * k + lane;
-            v[k] = row_of(ids[min(i, p.tokens - 1)], p.vocab);
-            if (i >= end || (v[k] & mask) != mine) v[k] = -1;
-        }
-#pragma unroll
-        for (int k = 0; k < kSortAhead; ++k) {
-            uint64_t left = __ballot(v[k] >= 0);
-            while (left) {                            // the lanes of one row at a time
-                const int leader = __builtin_ctzll(left);
-                const int r = __builtin_amdgcn_readlane(v[k], leader);
-                const uint64_t same = __ballot(v[k] == r);
-                const int where = next[r >> blocks_log2];
-                if (v[k] == r) {
-                    const int o = where + __builtin_popcountll(same & ((1ull << lane) - 1));
-                    p.place[o] = (int)(t + 64 * k + lane);
-                    p.row[o] = r;
-                }
-                if (lane == leader) next[r >> blocks_log2] = where + __builtin_popcountll(same);
-                left &= ~same;
+    // the groups that have some of the block's rows again, the next one's ids on their way
+    volatile int* next = counts + base;              // of this wave alone
+    auto id_of = [&](int g) { return ids[min(begin + 64L * g + lane, end - 1)]; };
+    const int groups = (int)((end - begin + 63) >> 6);
+    auto later = [&](int g) {                        // the first group from g on that may have some
+        while (g < groups && !(hits >> (g >> span_log2) & 1)) g = ((g >> span_log2) + 1) << span_log2;
+        return g;
+    };
+    int g = later(0);
+    I ahead = g < groups ? id_of(g) : (I)0;
+    while (g < groups) {
+        const long t0 = begin + 64L * g;
+        const unsigned v = t0 + lane < end ? sort_row(ahead, p.vocab) : 0xffffffffu;
+        g = later(g + 1);
+        if (g < groups) ahead = id_of(g);
+        uint64_t left = __ballot((v & mask_none) == mine);
+        while (left) {                                // the lanes of one row at a time
+            const int leader = __builtin_ctzll(left);
+            const unsigned r = __builtin_amdgcn_readlane(v, leader);
+            const uint64_t same = __ballot(v == r);
+            const int where = next[r >> blocks_log2];
+            if (v == r) {
+                const int o = where + __builtin_popcountll(same & ((1ull << lane) - 1));
+                p.place[o] = (int)(t0 + lane);
+                p.row[o] = (int)r;
             }
+            if (lane == leader) next[r >> blocks_log2] = where + __builtin_popcountll(same);
+            left &= ~same;
         }
     }
 }
@@ -169,6 +244,7 @@ __global__ __launch_bounds__(64 * kSortWaves) void embed_sort_kernel(const Embed
 // rows that no token has.
 constexpr int kPiece = 32;
 constexpr int kPieceAhead = 8;
+constexpr int kJoinWaves = 8;
 constexpr int kZeroRows = 16;              // rows that such a wave looks at
 
 template <typename T, int E>
@@ -246,11 +322,11 @@ __global__ __launch_bounds__(256) void embed_pieces_kernel(const EmbedParams p, 
 }
 
 // The rows whose tokens lie in several pieces: the piece in which they begin finds them by its last token and
-// adds the others' sums, four waves a share each, in a fixed order.
+// adds the others' sums, eight waves a share each, in a fixed order.
 template <typename T, int E>
-__global__ __launch_bounds__(256) void embed_join_kernel(const EmbedParams p)
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const EmbedParams p)
 {
-    __shared__ float sums[3][64][E];
+    __shared__ float sums[kJoinWaves - 1][64][E];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int dim = p.dim, packs = (dim + E - 1) / E;
     const int piece = blockIdx.x, last = (piece + 1) * kPiece - 1, valid = *p.valid;
@@ -262,7 +338,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const EmbedParams p)
     const uint64_t same = __ballot(lane < kPiece && p.row[piece * kPiece + (lane & (kPiece - 1))] == row);
     const int begin = piece * kPiece + __builtin_ctzll(same);
     const int end_piece = (begin + p.count[row] - 1) / kPiece;        // the last piece that has some of it
-    const int share = (end_piece - piece + 3) / 4;
+    const int share = (end_piece - piece + kJoinWaves - 1) / kJoinWaves;
     const int from = piece + 1 + wave * share, to = min(from + share, end_piece + 1);
     const int c = blockIdx.y * 64 + lane;
     const int col = column_of<E>(min(c, packs - 1), dim);
@@ -272,7 +348,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const EmbedParams p)
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] = tail[e];
     }
-#pragma unroll 4
+#pragma unroll 8
     for (int q = from; q < to; ++q) {
         const Pack<float, E> part = *reinterpret_cast<const Pack<float, E>*>(p.part + (long)q * 2 * dim + col);
 #pragma unroll
@@ -284,7 +360,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const EmbedParams p)
     }
     __syncthreads();
     if (wave || c >= packs) return;
-    for (int w = 0; w < 3; ++w)
+    for (int w = 0; w < kJoinWaves - 1; ++w)
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] += sums[w][lane][e];
     write_row<T, E>(p, row, col, acc);
@@ -312,15 +388,34 @@ hipError_t launch_sums(const EmbedParams& p, hipStream_t stream)
     embed_pieces_kernel<T, E><<<(unsigned)((tasks + 3) / 4), 256, 0, stream>>>(p, pieces, tiles);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || pieces < 2) return e;
-    embed_join_kernel<T, E><<<dim3(pieces - 1, tiles), 256, 0, stream>>>(p);
+    embed_join_kernel<T, E><<<dim3(pieces - 1, tiles), 64 * kJoinWaves, 0, stream>>>(p);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t embed_bwd_bytes(const EmbedParams& p)
+size_t embed_bwd_bytes(const EmbedParams& q)
 {
-    return ((size_t)p.tokens * 2 + p.vocab + 1 + (size_t)pieces_of(p) * 2 * p.dim) * 4;
+    EmbedParams p = q;
+    sort_shape(p);
+    const size_t shares = p.shares > 1 ? ((size_t)p.shares << p.blocks_log2) * (1 + sort_rows(p)) : 0;
+    return ((size_t)p.tokens * 2 + p.vocab + 1 + shares + (size_t)pieces_of(p) * 2 * p.dim) * 4;
+}
+
+template <typename I>
+static hipError_t launch_sort(const EmbedParams& p, hipStream_t stream)
+{
+    const dim3 grid(1 << p.blocks_log2, p.shares), block(64 * kSortWaves);
+    const size_t lds = (size_t)(sort_rows(p) * kSortWaves + 64) * sizeof(int);
+    if (p.shares == 1) {
+        embed_sort_kernel<I, Sort::all><<<grid, block, lds, stream>>>(p);
+        return hipGetLastError();
+    }
+    embed_sort_kernel<I, Sort::count><<<grid, block, lds, stream>>>(p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    embed_sort_kernel<I, Sort::place><<<grid, block, lds, stream>>>(p);
+    return hipGetLastError();
 }
 
 hipError_t launch_embed_fwd(const EmbedParams& p, hipStream_t stream)
@@ -336,11 +431,10 @@ hipError_t launch_embed_bwd(EmbedParams p, void* workspace, hipStream_t stream)
     p.row = p.place + p.tokens;
     p.count = p.row + p.tokens;
     p.valid = p.count + p.vocab;
-    const int log2 = sort_blocks_log2(p.vocab);
-    const size_t lds = (size_t)((p.vocab + (1 << log2) - 1) >> log2) * kSortWaves * sizeof(int);
-    if (p.wide_ids) embed_sort_kernel<int64_t><<<1 << log2, 64 * kSortWaves, lds, stream>>>(p, log2);
-    else embed_sort_kernel<int32_t><<<1 << log2, 64 * kSortWaves, lds, stream>>>(p, log2);
-    hipError_t e = hipGetLastError();
+    p.share_total = p.valid + 1;
+    sort_shape(p);
+    p.share_count = p.share_total + ((size_t)p.shares << p.blocks_log2);
+    const hipError_t e = p.wide_ids ? launch_sort<int64_t>(p, stream) : launch_sort<int32_t>(p, stream);
     if (e != hipSuccess) return e;
     if (p.dtype == 0) return p.dim < 4 ? launch_sums<float, 1>(p, stream) : launch_sums<float, 4>(p, stream);
     return p.dim < 8 ? launch_sums<bf16_t, 1>(p, stream) : launch_sums<bf16_t, 8>(p, stream);

@@ -12,8 +12,10 @@ __global__ __launch_bounds__(256) void gated_decay_kernel(const float* __restric
 {
     __shared__ float part[16][17];
     const int lane = threadIdx.x & 15, group = threadIdx.x >> 4, d = blockIdx.x * 16 + lane;
-    float s = 0.0f;
+    float s = 0.0f, slope = 0.0f, soft = 1.0f, own = 0.0f;
     if (d < dim) {
+        own = decay[d];
+        soft = softplus_f32(own, slope);
 #pragma unroll 4
         for (int k = group; k < shares; k += 16) s += qsum[(long)k * dim + d];
     }
@@ -22,10 +24,8 @@ __global__ __launch_bounds__(256) void gated_decay_kernel(const float* __restric
     if (group || d >= dim) return;
 #pragma unroll
     for (int g = 1; g < 16; ++g) s += part[g][lane];
-    float slope;
-    const float soft = softplus_f32(decay[d], slope);
     // (both go with e^decay where it is small, down to where they underflow)
-    ddecay[d] = s * (decay[d] < -16.0f ? 1.0f : slope / soft);
+    ddecay[d] = s * (own < -16.0f ? 1.0f : slope / soft);
 }
 
 hipError_t launch_kernels(const GatedParams& p, GatedPass pass, hipStream_t stream)
