@@ -166,16 +166,29 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_fwd_kernel(const N
     }
 }
 
+// Teams of a block: as many as four waves hold, so that few blocks (whose shares of dweight and dbias are written
+// and read once more) keep many rows in flight.
+template <int G, int W> constexpr int kBwdTeams = W == 1 ? 4 * (64 / G) : W == 2 ? 2 : 1;
+template <int W> constexpr int kBwdThreads = W <= 4 ? 256 : 64 * W;
+
+// Rows whose loads are under way beside the present one.  With two tensors of 2 bytes one row does not cover the
+// latency of memory, two do; teams of two and four waves lose more by the registers.  MI355X, us, gradients of
+// bf16 rows, one / two: 32768 x 768 36.5 / 34.7, 2048 x 8192 37.1 / 34.1, 8000 x 1025 22.5 / 24.6,
+// 4096 x 4096 33.9 / 34.7.
+template <typename T, bool RES, int W, int P>
+constexpr int kBwdAhead = P > 16 ? 0 : sizeof(T) == 2 && !RES && (W == 1 || W == 8) ? 2 : 1;
+
 template <typename T, bool RES, int E, int G, int W, int NV>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_bwd_kernel(const NormParams p)
+__global__ __launch_bounds__(kBwdThreads<W>) void norm_bwd_kernel(const NormParams p)
 {
     using Team = NormTeam<G, W, E * NV>;
+    constexpr int kTeams = kBwdTeams<G, W>;
     using S = std::conditional_t<RES, float, T>;
-    __shared__ float slots[2][2][W];
-    __shared__ float fold[W == 1 && G == 64 ? 3 * 64 * NV * E * 2 : 1];
+    __shared__ float slots[2][2][kTeams * W];
+    __shared__ float fold[kTeams > 1 && G == 64 ? (kTeams - 1) * 64 * W * NV * E * 2 : 1];
     const int dim = p.dim;
-    const int member = W == 1 ? threadIdx.x & (G - 1) : threadIdx.x;
-    const int team = W > 1 ? 0 : G == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x / G;
+    const int member = threadIdx.x & (G * W - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int team = G == 64 ? wave / W : threadIdx.x / G;
     const float scale = 1.0f / (float)dim;
     const bool whole = dim == Team::kLanes * E * NV;
     const S* s_in = RES ? reinterpret_cast<const S*>(p.sum) : static_cast<const S*>(p.x);
@@ -188,65 +201,81 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_bwd_kernel(const N
         for (int e = 0; e < E; ++e) { w[c][e] = 1.0f; dw[c][e] = 0.0f; db[c][e] = 0.0f; }
         if (p.weight) get<float, E>(p.weight + at.col, w[c]);
     }
-    const long step = (long)gridDim.x * Team::kRows;
-    long row = (long)blockIdx.x * Team::kRows + team;
-    Pack<S, E> qs[NV];
-    Pack<T, E> qy[NV];
+    const long step = (long)gridDim.x * kTeams;
+    long row = (long)blockIdx.x * kTeams + team;
+    // teams that meet at a barrier take the same number of rows, the last of them perhaps one that is not there
+    constexpr bool kTogether = W > 1 && kTeams > 1;
+    const long end = kTogether ? (p.rows + kTeams - 1) / kTeams * kTeams : p.rows;
+    constexpr int kAhead = kBwdAhead<T, RES, W, E * NV>, kRows = kAhead > 1 ? 2 : 1;
+    struct Row {
+        Pack<S, E> s[NV];
+        Pack<T, E> y[NV];
+        float mean, rstd;
+    };
+    Row held[kRows];
     Pack<float, E> qd[NV];
-    float mean = 0.0f, rstd = 0.0f;
-    auto fetch = [&](long r) {
+    auto fetch = [&](long r, Row& q) {
+        if (kTogether || kAhead > 1) r = min(r, p.rows - 1);
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             const Columns<E> at(c * Team::kLanes + member, dim);
-            qs[c] = *reinterpret_cast<const Pack<S, E>*>(s_in + r * dim + at.col);
-            qy[c] = *reinterpret_cast<const Pack<T, E>*>(static_cast<const T*>(p.dy) + r * dim + at.col);
-            if constexpr (RES && Team::kAhead)
+            q.s[c] = *reinterpret_cast<const Pack<S, E>*>(s_in + r * dim + at.col);
+            q.y[c] = *reinterpret_cast<const Pack<T, E>*>(static_cast<const T*>(p.dy) + r * dim + at.col);
+            if constexpr (RES && kAhead)
                 if (p.dsum) qd[c] = *reinterpret_cast<const Pack<float, E>*>(p.dsum + r * dim + at.col);
         }
-        mean = p.mean[r];
-        rstd = p.rstd[r];
+        q.mean = p.mean[r];
+        q.rstd = p.rstd[r];
     };
-    if (Team::kAhead && row < p.rows) fetch(row);
-    for (int parity = 0; row < p.rows; row += step, parity ^= 1) {
-        if (!Team::kAhead) fetch(row);
+    if (kAhead && row < end) fetch(row, held[0]);
+    if (kAhead > 1 && row < end) fetch(row + step, held[kRows - 1]);
+    for (int parity = 0; row < end; row += step, parity ^= 1) {
+        if (!kAhead) fetch(row, held[0]);
+        const bool there = !kTogether || row < p.rows;
         float hat[NV][E], g[NV][E], d[NV][E];
         float sum_g = 0.0f, sum_gh = 0.0f;
-        const float rs = rstd;
+        const float rs = held[0].rstd, mean = held[0].mean;
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             const Columns<E> at(c * Team::kLanes + member, dim);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const bool in = whole || at.in(e, dim);
-                const float dy = to_f32(qy[c].v[e]);
-                hat[c][e] = (to_f32(qs[c].v[e]) - mean) * rs;
+                const bool in = (whole || at.in(e, dim)) && there;
+                const float dy = to_f32(held[0].y[c].v[e]);
+                hat[c][e] = (to_f32(held[0].s[c].v[e]) - mean) * rs;
                 g[c][e] = dy * w[c][e];
-                if (Team::kAhead) d[c][e] = RES && p.dsum ? qd[c].v[e] : 0.0f;
+                if (kAhead) d[c][e] = RES && p.dsum ? qd[c].v[e] : 0.0f;
                 sum_g += in ? g[c][e] : 0.0f;
                 sum_gh += in ? g[c][e] * hat[c][e] : 0.0f;
                 dw[c][e] += in ? dy * hat[c][e] : 0.0f;
                 db[c][e] += in ? dy : 0.0f;
             }
         }
-        if (Team::kAhead && row + step < p.rows) fetch(row + step);
+        if constexpr (kAhead > 1) {
+            held[0] = held[1];
+            if (row + step < end) fetch(row + 2 * step, held[1]);
+        } else if (kAhead && row + step < end) {
+            fetch(row + step, held[0]);
+        }
         sum_g = lanes_sum<G>(sum_g);
         sum_gh = lanes_sum<G>(sum_gh);
         if constexpr (W > 1) {
             if ((threadIdx.x & 63) == 0) {
-                slots[parity][0][threadIdx.x >> 6] = sum_g;
-                slots[parity][1][threadIdx.x >> 6] = sum_gh;
+                slots[parity][0][wave] = sum_g;
+                slots[parity][1][wave] = sum_gh;
             }
             __syncthreads();
             sum_g = sum_gh = 0.0f;
 #pragma unroll
-            for (int v = 0; v < W; ++v) { sum_g += slots[parity][0][v]; sum_gh += slots[parity][1][v]; }
+            for (int v = 0; v < W; ++v) { sum_g += slots[parity][0][team * W + v]; sum_gh += slots[parity][1][team * W + v]; }
         }
         sum_g *= scale;
         sum_gh *= scale;
+        if (!there) continue;
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             const Columns<E> at(c * Team::kLanes + member, dim);
-            if constexpr (!Team::kAhead) {
+            if constexpr (!kAhead) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) d[c][e] = 0.0f;
                 if constexpr (RES)
@@ -263,14 +292,15 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_bwd_kernel(const N
     // the block's share of dweight and dbias: its teams' sums, added in a fixed order
     float* part_w = p.part + (long)blockIdx.x * 2 * dim;
     float* part_b = part_w + dim;
-    if constexpr (W == 1 && G == 64) {
+    if constexpr (kTeams > 1 && G == 64) {
+        constexpr int L = 64 * W;
         if (team > 0) {
 #pragma unroll
             for (int c = 0; c < NV; ++c)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    fold[(((team - 1) * NV + c) * 2 * E + e) * 64 + member] = dw[c][e];
-                    fold[(((team - 1) * NV + c) * 2 * E + E + e) * 64 + member] = db[c][e];
+                    fold[(((team - 1) * NV + c) * 2 * E + e) * L + member] = dw[c][e];
+                    fold[(((team - 1) * NV + c) * 2 * E + E + e) * L + member] = db[c][e];
                 }
         }
         __syncthreads();
@@ -280,9 +310,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_bwd_kernel(const N
 #pragma unroll
             for (int e = 0; e < E; ++e)
 #pragma unroll 1
-                for (int t = 0; t < 3; ++t) {
-                    dw[c][e] += fold[((t * NV + c) * 2 * E + e) * 64 + member];
-                    db[c][e] += fold[((t * NV + c) * 2 * E + E + e) * 64 + member];
+                for (int t = 0; t < kTeams - 1; ++t) {
+                    dw[c][e] += fold[((t * NV + c) * 2 * E + e) * L + member];
+                    db[c][e] += fold[((t * NV + c) * 2 * E + E + e) * L + member];
                 }
     } else if constexpr (G == 16) {
         __shared__ float small[16 * 16 * NV * E * 2];
@@ -448,13 +478,13 @@ NormShape norm_shape(const NormParams& p)
     s.packs = 0;
     return s;
 }
-// Teams of a block.
+// Teams of a block, forward.
 int norm_block_rows(const NormShape& s) { return s.packs == 0 || s.waves > 1 ? 1 : 4 * (64 / s.lanes); }
 
 template <typename T, bool RES, int E, int G, int W, int NV>
 hipError_t launch_shape(const NormParams& p, bool backward, unsigned blocks, hipStream_t stream)
 {
-    if (backward) norm_bwd_kernel<T, RES, E, G, W, NV><<<blocks, W == 1 ? 256 : 64 * W, 0, stream>>>(p);
+    if (backward) norm_bwd_kernel<T, RES, E, G, W, NV><<<blocks, kBwdThreads<W>, 0, stream>>>(p);
     else norm_fwd_kernel<T, RES, E, G, W, NV><<<blocks, W == 1 ? 256 : 64 * W, 0, stream>>>(p);
     return hipGetLastError();
 }
@@ -504,13 +534,16 @@ hipError_t launch(const NormParams& p, bool backward, hipStream_t stream)
         return p.with_residual ? launch_typed<float, true>(p, backward, stream) : launch_typed<float, false>(p, backward, stream);
     return p.with_residual ? launch_typed<bf16_t, true>(p, backward, stream) : launch_typed<bf16_t, false>(p, backward, stream);
 }
-// Blocks of the backward kernel, each with a share of dweight and dbias.
+// Blocks of the backward kernel, each with a share of dweight and dbias.  MI355X, us, blocks 256 / 512 / 768 / 1024:
+// 32768 x 768 bf16 with a residual 99.4 / 80.1 / 92.5 / 86.2, 25216 x 384 fp32 31.3 / 25.5 / 28.0 / 27.9,
+// 8000 x 1025 bf16 27.7 / 22.5 / 24.6 / 25.8, 4096 x 4096 bf16 37.9 / 33.9 / 39.4 / 47.6.  Teams of eight waves: one
+// a CU.
 int norm_shares(const NormParams& p)
 {
     const NormShape s = norm_shape(p);
-    const int per = norm_block_rows(s);
+    const int per = s.packs == 0 ? 1 : s.waves == 1 ? 4 * (64 / s.lanes) : s.waves == 2 ? 2 : 1;
     const long whole = (p.rows + per - 1) / per;
-    const long most = s.waves >= 8 || s.packs == 0 ? 256 : 512;
+    const long most = s.waves == 8 || s.packs == 0 ? 256 : 512;
     return (int)(whole < most ? whole : most);
 }
 
