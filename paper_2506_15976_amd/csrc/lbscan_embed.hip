@@ -56,15 +56,16 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const EmbedParams p)
 // ---- gradient: the tokens sorted by row ------------------------------------------------------------
 // A stable counting sort.  Block (r, c) has the rows v = r mod R, R a power of two (so that rows that are used much and
 // lie next to each other in a table ordered by frequency go to different blocks), and the c-th share of the
-// tokens.  It looks at every id of its share and counts those of its rows, by row and by sixteenth of the share (a
+// tokens.  It looks at every id of its share and counts those of its rows, by row and by eighth of the share (a
 // wave each).  Running sums of the counts over rows, shares and waves say where each wave puts its tokens; a wave takes
 // them in order, so that the tokens of a row stay in theirs.  One share: one launch, in which a block also
 // counts the tokens of the blocks before it.  Several: a launch that counts and one that places, since what
-// takes the time is one wave walking through the tokens of a much used row.  MI355X, us, Zipf's law over 50000 rows,
-// the call with one share and with eight: 32768 x 768 bf16
-// 48.3 / 43.6, 65536 x 512 bf16 over 300 rows 63.7 / 42.7.
-constexpr int kSortWaves = 16;
-constexpr int kSortRows = 896;             // most rows of a block: 56 KB of counts, and a thread each
+// takes the time is one wave walking through the tokens of a much used row.  More than eight lose by the counts of the
+// other shares that every block reads.  MI355X, us, the gradient of 32768 x 768 bf16 by Zipf's law over 50000 rows: one
+// share 48.3, eight 44.6, sixteen 52.9; of 65536 x 512 bf16 over 300 rows 63.7, 43.2, 46.9.
+constexpr int kSortWaves = 8;
+constexpr int kSortThreads = 64 * kSortWaves;
+constexpr int kSortRows = 2 * kSortThreads;   // most rows of a block: two to a thread, 32 KB of counts
 constexpr int kSortShare = 4096;           // tokens of a share, where the grid allows
 constexpr int kSortShares = 8;             // most shares: two blocks a CU where there are 64 of rows
 constexpr int kSortAhead = 4;              // groups of 64 ids that a wave loads together at first
@@ -104,7 +105,7 @@ __device__ __forceinline__ int block_sum(int v, int (&totals)[kSortWaves])
 }
 
 template <typename I, Sort WHAT>
-__global__ __launch_bounds__(64 * kSortWaves) void embed_sort_kernel(const EmbedParams p)
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedParams p)
 {
     extern __shared__ int counts[];        // (waves, rows), and a place per lane for what does not count
     __shared__ int totals[kSortWaves];
@@ -124,23 +125,27 @@ __global__ __launch_bounds__(64 * kSortWaves) void embed_sort_kernel(const Embed
     while ((share >> 6 >> span_log2) > 64) ++span_log2;
     uint64_t hits = 0;
 
-    // what the launch before left is on its way meanwhile: a thread a row; `all`: over all shares, `before`: over those
-    // before this one
-    const int row = threadIdx.x, row_pitch = ((unsigned)p.vocab + mask) >> blocks_log2;
-    int all = 0, before = 0, below = 0;
+    // What the launch before left is on its way meanwhile.  A thread has the rows threadIdx.x and, of many,
+    // threadIdx.x + kSortThreads; `all`: their tokens in all shares, `before`: in those before this one.
+    const int row_pitch = (int)(((unsigned)p.vocab + mask) >> blocks_log2);
+    int all[2] = {0, 0}, before[2] = {0, 0}, below = 0;
     if constexpr (WHAT == Sort::place) {
-        const int* of_row = p.share_count + (long)mine * row_pitch + min(row, rows - 1);
 #pragma unroll
-        for (unsigned c = 0; c < kSortShares; ++c) {
-            const int v = c < gridDim.y ? of_row[(long)c * gridDim.x * row_pitch] : 0;
-            before += c < blockIdx.y ? v : 0;
-            all += v;
+        for (int k = 0; k < 2; ++k) {
+            const int row = threadIdx.x + k * kSortThreads;
+            if (k && rows <= kSortThreads) break;
+            const int* of_row = p.share_count + (long)mine * row_pitch + min(row, rows - 1);
+#pragma unroll
+            for (unsigned c = 0; c < kSortShares; ++c) {
+                const int v = c < gridDim.y ? of_row[(long)c * gridDim.x * row_pitch] : 0;
+                before[k] += c < blockIdx.y ? v : 0;
+                all[k] += v;
+            }
+            if (row >= rows) all[k] = before[k] = 0;
         }
-        if (row >= rows) all = before = 0;
-        static_assert(kSortShares << 6 <= 64 * kSortWaves);
-        if (threadIdx.x < gridDim.x * gridDim.y) below = (threadIdx.x & mask) < mine ? p.share_total[threadIdx.x] : 0;
+        for (unsigned k = threadIdx.x; k < gridDim.x * gridDim.y; k += kSortThreads) below += (k & mask) < mine ? p.share_total[k] : 0;
     }
-    for (int k = threadIdx.x; k < rows * kSortWaves; k += 64 * kSortWaves) counts[k] = 0;
+    for (int k = threadIdx.x; k < rows * kSortWaves; k += kSortThreads) counts[k] = 0;
     __syncthreads();
     // Every block looks at every id: whole groups are loaded without a check, and no lane waits for a branch (ids of
     // other blocks are counted where nobody looks).
@@ -169,40 +174,53 @@ __global__ __launch_bounds__(64 * kSortWaves) void embed_sort_kernel(const Embed
     __syncthreads();
 
     // running sums, rows first
-    int n = 0;
-    if (row < rows)
+    int n[2] = {0, 0};
 #pragma unroll
-        for (int w = 0; w < kSortWaves; ++w) n += counts[w * rows + row];
+    for (int k = 0; k < 2; ++k) {
+        const int row = threadIdx.x + k * kSortThreads;
+        if (row < rows) {
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) n[k] += counts[w * rows + row];
+            if (WHAT == Sort::count) p.share_count[((long)blockIdx.y * gridDim.x + mine) * row_pitch + row] = n[k];
+        }
+    }
     if constexpr (WHAT == Sort::count) {
-        if (row < rows) p.share_count[((long)blockIdx.y * gridDim.x + mine) * row_pitch + row] = n;
-        n = block_sum(n, totals);
-        if (threadIdx.x == 0) p.share_total[blockIdx.y * gridDim.x + mine] = n;
+        const int own = block_sum(n[0] + n[1], totals);
+        if (threadIdx.x == 0) p.share_total[blockIdx.y * gridDim.x + mine] = own;
         return;
     }
-    if (WHAT == Sort::all) all = n;
-    below = block_sum(below, totals);
-    if (row < rows && blockIdx.y == 0) p.count[mine + ((unsigned)row << blocks_log2)] = all;
-    int sum = all;
+    int first = block_sum(below, totals);            // where the block's rows begin
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        const int other = __shfl_up(sum, m);
-        if (lane >= m) sum += other;
-    }
-    __syncthreads();
-    if (lane == 63) totals[wave] = sum;
-    __syncthreads();
-    int at = below + sum - all + before, own = 0;
-    for (int w = 0; w < kSortWaves; ++w) {
-        if (w < wave) at += totals[w];
-        own += totals[w];
-    }
-    if (row < rows)
-        for (int w = 0; w < kSortWaves; ++w) {
-            const int c = counts[w * rows + row];
-            counts[w * rows + row] = at;
-            at += c;
+    for (int k = 0; k < 2; ++k) {
+        if (k && rows <= kSortThreads) break;
+        const int row = threadIdx.x + k * kSortThreads;
+        if (WHAT == Sort::all) all[k] = n[k];
+        if (row < rows && blockIdx.y == 0) p.count[mine + ((unsigned)row << blocks_log2)] = all[k];
+        int sum = all[k];
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) {
+            const int other = __shfl_up(sum, m);
+            if (lane >= m) sum += other;
         }
-    if (mine == mask && blockIdx.y == 0 && threadIdx.x == 0) *p.valid = below + own;
+        __syncthreads();
+        if (lane == 63) totals[wave] = sum;
+        __syncthreads();
+        int at = first + sum - all[k] + before[k];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) {
+            if (w < wave) at += totals[w];
+            first += totals[w];
+        }
+        if (row < rows) {
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) {
+                const int c = counts[w * rows + row];
+                counts[w * rows + row] = at;
+                at += c;
+            }
+        }
+    }
+    if (mine == mask && blockIdx.y == 0 && threadIdx.x == 0) *p.valid = first;
     __syncthreads();
 
     // the groups that have some of the block's rows again, the next one's ids on their way
@@ -405,7 +423,7 @@ size_t embed_bwd_bytes(const EmbedParams& q)
 template <typename I>
 static hipError_t launch_sort(const EmbedParams& p, hipStream_t stream)
 {
-    const dim3 grid(1 << p.blocks_log2, p.shares), block(64 * kSortWaves);
+    const dim3 grid(1 << p.blocks_log2, p.shares), block(kSortThreads);
     const size_t lds = (size_t)(sort_rows(p) * kSortWaves + 64) * sizeof(int);
     if (p.shares == 1) {
         embed_sort_kernel<I, Sort::all><<<grid, block, lds, stream>>>(p);
