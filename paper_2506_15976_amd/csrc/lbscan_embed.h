@@ -27,6 +27,7 @@ struct EmbedParams {
     int* share_total;         // tokens of (share of the tokens, block of rows), and of each of its rows
     int* share_count;
     int blocks_log2, shares;  // the sort's grid
+    int piece;                // sorted tokens that a wave adds
     float* part;              // (pieces, 2, dim)
 };
 

@@ -104,19 +104,58 @@ __device__ __forceinline__ int block_sum(int v, int (&totals)[kSortWaves])
     return v;
 }
 
+// Zeros to the rows of dweight that no token has: a wave looks at kZeroRows rows.  These blocks stand behind those that
+// sort, in the same launch: the sort waits for memory and leaves its rate to them.  With one share the counts are
+// not there yet, and every row is set to zero; the sums overwrite the few that have tokens.
+constexpr int kZeroRows = 16;
+constexpr int kZeroBlock = kZeroRows * kSortWaves;
+struct __attribute__((packed, aligned(2))) Zeros { uint32_t w[4]; };
+
+__device__ __forceinline__ void zero_rows(const EmbedParams& p, long v0, bool counted, unsigned blocks, int row_pitch)
+{
+    if (v0 >= p.vocab) return;
+    const int lane = threadIdx.x & 63;
+    const unsigned v = (unsigned)min(v0 + (lane & (kZeroRows - 1)), (long)p.vocab - 1);
+    int tokens = 0;
+    if (counted) {
+        const int* of_row = p.share_count + (long)(v & (blocks - 1)) * row_pitch + (v >> p.blocks_log2);
+#pragma unroll
+        for (int c = 0; c < kSortShares; ++c) tokens += c < p.shares ? of_row[(long)c * blocks * row_pitch] : 0;
+    }
+    uint64_t empty = __ballot(lane < kZeroRows && v0 + lane < p.vocab && tokens == 0);
+    const long bytes = (long)p.dim * (p.dtype == 0 ? 4 : 2);
+    char* const table = static_cast<char*>(p.dweight);
+    while (empty) {
+        char* to = table + (v0 + __builtin_ctzll(empty)) * bytes;
+        empty &= empty - 1;
+        if (bytes >= 16) {
+            for (long c = 16L * lane; c < bytes; c += 16 * 64) *reinterpret_cast<Zeros*>(to + min(c, bytes - 16)) = Zeros{};
+        } else if (2 * lane < bytes) {
+            reinterpret_cast<uint16_t*>(to)[lane] = 0;
+        }
+    }
+}
+
 template <typename I, Sort WHAT>
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedParams p)
 {
     extern __shared__ int counts[];        // (waves, rows), and a place per lane for what does not count
     __shared__ int totals[kSortWaves];
     const int blocks_log2 = p.blocks_log2;
+    if (WHAT != Sort::count && (int)blockIdx.y >= p.shares) {
+        const long block = (long)(blockIdx.y - p.shares) * gridDim.x + blockIdx.x;
+        zero_rows(p, block * kZeroBlock + (threadIdx.x >> 6) * kZeroRows, WHAT == Sort::place, gridDim.x,
+                  (int)(((unsigned)p.vocab + (1u << blocks_log2) - 1) >> blocks_log2));
+        return;
+    }
+    const unsigned shares = p.shares;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned mine = blockIdx.x, mask = (1u << blocks_log2) - 1;
     const unsigned mask_none = mask | 0x80000000u;
     const int rows = (int)(((unsigned)p.vocab + mask - mine) >> blocks_log2);   // v = mine + k * blocks < vocab
     const I* ids = static_cast<const I*>(p.ids);
     // the block's share of the tokens, and the wave's of that: whole groups of 64
-    const long block_share = ((p.tokens + gridDim.y - 1) / gridDim.y + 63) / 64 * 64;
+    const long block_share = ((p.tokens + shares - 1) / shares + 63) / 64 * 64;
     const long block_begin = min(block_share * blockIdx.y, p.tokens), block_end = min(block_begin + block_share, p.tokens);
     const long share = ((block_end - block_begin + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
     const long begin = min(block_begin + share * wave, block_end), end = min(begin + share, block_end);
@@ -137,13 +176,13 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedPar
             const int* of_row = p.share_count + (long)mine * row_pitch + min(row, rows - 1);
 #pragma unroll
             for (unsigned c = 0; c < kSortShares; ++c) {
-                const int v = c < gridDim.y ? of_row[(long)c * gridDim.x * row_pitch] : 0;
+                const int v = c < shares ? of_row[(long)c * gridDim.x * row_pitch] : 0;
                 before[k] += c < blockIdx.y ? v : 0;
                 all[k] += v;
             }
             if (row >= rows) all[k] = before[k] = 0;
         }
-        for (unsigned k = threadIdx.x; k < gridDim.x * gridDim.y; k += kSortThreads) below += (k & mask) < mine ? p.share_total[k] : 0;
+        for (unsigned k = threadIdx.x; k < gridDim.x * shares; k += kSortThreads) below += (k & mask) < mine ? p.share_total[k] : 0;
     }
     for (int k = threadIdx.x; k < rows * kSortWaves; k += kSortThreads) counts[k] = 0;
     __syncthreads();
@@ -256,14 +295,15 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedPar
 }
 
 // ---- gradient: sums over the sorted tokens -----------------------------------------------------------
-// A wave takes a piece of kPiece sorted tokens and 64 packs of columns, and adds dout row by row.  A row of the
+// A wave takes a piece of the sorted tokens and 64 packs of columns, and adds dout row by row.  A row of the
 // table whose tokens all lie in the piece is written; of others the sum goes to scratch: [0] of a row that
-// began in an earlier piece, [1] of one that begins here and goes on.  The waves behind the pieces write zeros to the
-// rows that no token has.
-constexpr int kPiece = 32;
+// began in an earlier piece, [1] of one that begins here and goes on.
+// Few tokens: short pieces, as what counts is how long a wave takes; many: long ones, as every piece costs a block that
+// looks for rows to join.  MI355X, us, the gradient with pieces of 8 / 16 / 32: 256 x 256 of 2000 rows 12.2 / 12.7 / 15.7,
+// 4096 x 768 of 50000 24.5 / 25.1 / 28.6, 16384 x 2048 of 50000 68.4 / 62.7 / 60.4, 32768 x 768 48.9 / 43.7 / 43.2.
+int piece_of(long tokens) { return tokens <= 4096 ? 8 : tokens <= 8192 ? 16 : 32; }
 constexpr int kPieceAhead = 8;
 constexpr int kJoinWaves = 8;
-constexpr int kZeroRows = 16;              // rows that such a wave looks at
 
 template <typename T, int E>
 __device__ __forceinline__ void write_row(const EmbedParams& p, int row, int col, const float acc[E])
@@ -280,21 +320,9 @@ __global__ __launch_bounds__(256) void embed_pieces_kernel(const EmbedParams p, 
     const int lane = threadIdx.x & 63;
     const unsigned task = blockIdx.x * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int dim = p.dim, packs = (dim + E - 1) / E;
-    if (task >= pieces * tiles) {
-        const long v0 = (long)(task - pieces * tiles) * kZeroRows;
-        if (v0 >= p.vocab) return;
-        const int v = (int)v0 + (lane & (kZeroRows - 1));
-        uint64_t empty = __ballot(lane < kZeroRows && v < p.vocab && p.count[min(v, p.vocab - 1)] == 0);
-        const float zeros[E] = {};
-        while (empty) {
-            const int k = __builtin_ctzll(empty);
-            empty &= empty - 1;
-            for (int c = lane; c < packs; c += 64) write_row<T, E>(p, (int)v0 + k, column_of<E>(c, dim), zeros);
-        }
-        return;
-    }
+    if (task >= pieces * tiles) return;
     const int piece = (int)(task / tiles), c = (int)(task % tiles) * 64 + lane;
-    const int valid = *p.valid, first = piece * kPiece, n = min(kPiece, valid - first);
+    const int valid = *p.valid, first = piece * p.piece, n = min(p.piece, valid - first);
     if (n <= 0) return;
     const bool there = c < packs;
     const int col = column_of<E>(min(c, packs - 1), dim);
@@ -302,8 +330,13 @@ __global__ __launch_bounds__(256) void embed_pieces_kernel(const EmbedParams p, 
     const int row_before = first > 0 ? p.row[first - 1] : -1, row_after = first + n < valid ? p.row[first + n] : -1;
     const T* dout = static_cast<const T*>(p.dout);
 
+    // bit k: the k-th token is the last of its row in the piece
+    const int my_next = __shfl_down(my_row, 1);
+    const uint64_t last = __ballot(lane < n && (lane == n - 1 || my_next != my_row));
+    const bool early = row_before == __builtin_amdgcn_readlane(my_row, 0);             // the first row began before
+    const bool goes_on = row_after == __builtin_amdgcn_readlane(my_row, n - 1);        // the last one goes on behind
+    const uint64_t first_row = last & -last;
     float acc[E] = {};
-    int begun = 0;                          // where the present row's tokens begin in the piece
     for (int k0 = 0; k0 < n; k0 += kPieceAhead) {
         Pack<T, E> q[kPieceAhead];
 #pragma unroll
@@ -313,27 +346,24 @@ __global__ __launch_bounds__(256) void embed_pieces_kernel(const EmbedParams p, 
         }
 #pragma unroll
         for (int k = 0; k < kPieceAhead; ++k) {
-            const int at = k0 + k;
-            if (at < n) {
-                const int row = __builtin_amdgcn_readlane(my_row, at);
-                const int follows = at + 1 < n ? __builtin_amdgcn_readlane(my_row, at + 1) : row_after;
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] += to_f32(q[k].v[e]);
-                if (row != follows || at + 1 == n) {
-                    const bool early = begun == 0 && row_before == row, goes_on = row == follows;
-                    if (there) {
-                        if (!early && !goes_on) {
-                            write_row<T, E>(p, row, col, acc);
-                        } else {
-                            float* to = p.part + ((long)piece * 2 + (early ? 0 : 1)) * dim + col;
+            for (int e = 0; e < E; ++e) acc[e] += to_f32(q[k].v[e]);
+            const uint64_t bit = 1ull << (k0 + k);
+            if (last & bit) {
+                const bool in_part = (early && (bit & first_row)) || (goes_on && k0 + k == n - 1);
+                if (there) {
+                    if (!in_part) {
+                        write_row<T, E>(p, __builtin_amdgcn_readlane(my_row, k0 + k), col, acc);
+                    } else {
+                        float* to = p.part + ((long)piece * 2 + (early && (bit & first_row) ? 0 : 1)) * dim + col;
+                        Pack<float, E> o;
 #pragma unroll
-                            for (int e = 0; e < E; ++e) to[e] = acc[e];
-                        }
+                        for (int e = 0; e < E; ++e) o.v[e] = acc[e];
+                        *reinterpret_cast<Pack<float, E>*>(to) = o;
                     }
-#pragma unroll
-                    for (int e = 0; e < E; ++e) acc[e] = 0.0f;
-                    begun = at + 1;
                 }
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = 0.0f;
             }
         }
     }
@@ -347,15 +377,15 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const Embed
     __shared__ float sums[kJoinWaves - 1][64][E];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int dim = p.dim, packs = (dim + E - 1) / E;
-    const int piece = blockIdx.x, last = (piece + 1) * kPiece - 1, valid = *p.valid;
+    const int piece = blockIdx.x, begins = piece * p.piece, last = begins + p.piece - 1, valid = *p.valid;
     if (last + 1 >= valid) return;                                     // nothing behind this piece
     const int row = p.row[last];
     if (p.row[last + 1] != row) return;
-    if (piece > 0 && p.row[piece * kPiece - 1] == row) return;        // it began earlier
+    if (piece > 0 && p.row[begins - 1] == row) return;        // it began earlier
     // first token of the row: lanes compare the piece's rows
-    const uint64_t same = __ballot(lane < kPiece && p.row[piece * kPiece + (lane & (kPiece - 1))] == row);
-    const int begin = piece * kPiece + __builtin_ctzll(same);
-    const int end_piece = (begin + p.count[row] - 1) / kPiece;        // the last piece that has some of it
+    const uint64_t same = __ballot(lane < p.piece && p.row[min(begins + lane, last)] == row);
+    const int begin = begins + __builtin_ctzll(same);
+    const int end_piece = (begin + p.count[row] - 1) / p.piece;        // the last piece that has some of it
     const int share = (end_piece - piece + kJoinWaves - 1) / kJoinWaves;
     const int from = piece + 1 + wave * share, to = min(from + share, end_piece + 1);
     const int c = blockIdx.y * 64 + lane;
@@ -384,7 +414,11 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const Embed
     write_row<T, E>(p, row, col, acc);
 }
 
-int pieces_of(const EmbedParams& p) { return (int)((p.tokens + kPiece - 1) / kPiece); }
+int pieces_of(const EmbedParams& p)
+{
+    const int piece = piece_of(p.tokens);
+    return (int)((p.tokens + piece - 1) / piece);
+}
 
 template <typename T, int E>
 hipError_t launch_fwd(const EmbedParams& p, hipStream_t stream)
@@ -401,7 +435,8 @@ template <typename T, int E>
 hipError_t launch_sums(const EmbedParams& p, hipStream_t stream)
 {
     const int pieces = pieces_of(p), packs = (p.dim + E - 1) / E, tiles = (packs + 63) / 64;
-    const long tasks = (long)pieces * tiles + ((long)p.vocab + kZeroRows - 1) / kZeroRows;
+    const long tasks = (long)pieces * tiles;
+    if (tasks == 0) return hipSuccess;
     if (tasks > 0x7fffffffL) return hipErrorInvalidValue;
     embed_pieces_kernel<T, E><<<(unsigned)((tasks + 3) / 4), 256, 0, stream>>>(p, pieces, tiles);
     hipError_t e = hipGetLastError();
@@ -425,14 +460,16 @@ static hipError_t launch_sort(const EmbedParams& p, hipStream_t stream)
 {
     const dim3 grid(1 << p.blocks_log2, p.shares), block(kSortThreads);
     const size_t lds = (size_t)(sort_rows(p) * kSortWaves + 64) * sizeof(int);
+    const long zeros = ((long)p.vocab + kZeroBlock - 1) / kZeroBlock;
+    const dim3 with_zeros(grid.x, (unsigned)(p.shares + (zeros + grid.x - 1) / grid.x));
     if (p.shares == 1) {
-        embed_sort_kernel<I, Sort::all><<<grid, block, lds, stream>>>(p);
+        embed_sort_kernel<I, Sort::all><<<with_zeros, block, lds, stream>>>(p);
         return hipGetLastError();
     }
     embed_sort_kernel<I, Sort::count><<<grid, block, lds, stream>>>(p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    embed_sort_kernel<I, Sort::place><<<grid, block, lds, stream>>>(p);
+    embed_sort_kernel<I, Sort::place><<<with_zeros, block, lds, stream>>>(p);
     return hipGetLastError();
 }
 
@@ -445,6 +482,7 @@ hipError_t launch_embed_fwd(const EmbedParams& p, hipStream_t stream)
 hipError_t launch_embed_bwd(EmbedParams p, void* workspace, hipStream_t stream)
 {
     p.part = static_cast<float*>(workspace);
+    p.piece = piece_of(p.tokens);
     p.place = reinterpret_cast<int*>(p.part + (size_t)pieces_of(p) * 2 * p.dim);
     p.row = p.place + p.tokens;
     p.count = p.row + p.tokens;
