@@ -1,5 +1,7 @@
 """Gated linear recurrence on the GPU against the 64-bit reference: every family of launch shapes, both directions,
 packed sequences, states in and out, gates that are closed, and what must not leak out of a masked past."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -74,6 +76,16 @@ def test_lengths(lb, L, reverse, dtype):
 @pytest.mark.parametrize("L", [1, 5, 8, 60, 100, 197, 300, 600, 1500, 9001])
 def test_packed_sequences(lb, L, reverse, dtype):
     t, more = make(3, 3, L, dtype, seed=2, starts=True)
+    check(lb, t, more, dtype, reverse)
+
+
+# few long rows, which are cut into pieces that several blocks take
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("L,starts", [(33000, False), (40001, True)])
+def test_cut_rows(lb, L, starts, reverse, dtype):
+    t, more = make(1, 3, L, dtype, seed=19, starts=starts)
+    assert lb.load().lbscan_gated_workspace_bytes(ctypes.byref(lb.LbscanGatedArgs(1, 3, L, int(dtype == "bf16"))), 0) > 0
     check(lb, t, more, dtype, reverse)
 
 
@@ -162,7 +174,7 @@ def test_decay_range(lb, decay):
 
 
 @pytest.mark.parametrize("reverse", [False, True])
-@pytest.mark.parametrize("L,cut", [(6, 3), (50, 20), (197, 100), (700, 333), (9001, 4500)])
+@pytest.mark.parametrize("L,cut", [(6, 3), (50, 20), (197, 100), (700, 333), (9001, 4500), (40001, 23456)])
 def test_a_start_keeps_the_past_out(lb, L, cut, reverse):
     """NaN and infinities before a start, in tokens and in the state, reach nothing behind it, nor do gradients
     behind a start reach what is before it."""
@@ -219,10 +231,9 @@ def test_steps_equal_the_prompt(lb, dtype):
     close(state, hT, GATED["fp32"], "state")
 
 
-@pytest.mark.parametrize("B,D,L", [(2, 3, 5), (2, 3, 50), (1, 300, 3000), (1, 3, 9001)])
+@pytest.mark.parametrize("B,D,L", [(2, 3, 5), (2, 3, 50), (1, 300, 3000), (1, 3, 9001), (1, 3, 50000)])
 def test_state_in_place(lb, B, D, L):
     """hT may be h0, also where a row is cut and every piece reads the state that enters."""
-    import ctypes
     from paper_2506_15976_amd import binding
     t, _ = make(B, D, L, seed=12)
     y, hT = lb.lbscan_gated_fwd(**t, return_state=True)
