@@ -79,7 +79,8 @@ def causal_conv1d_silu(x, weight, bias=None, *, activation=True, reverse=False):
 
 
 # The operators around the scan.  Their autograd nodes are in csrc/lbscan_torch.cpp: these calls are short, and
-# a node in Python costs more host time than their kernels take.
+# a node in Python costs more host time than their kernels take.  They can be differentiated once (a backward pass
+# with create_graph raises an error).
 
 def gated_linear_recurrence(x, gate_a, gate_x, decay, *, rate=8.0, starts=None, reverse=False, h0=None,
                             return_state=False):

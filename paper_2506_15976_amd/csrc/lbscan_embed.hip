@@ -1,5 +1,7 @@
 // Token embedding and its gradient (formulas: lbscan_embed.h).  All of it is bound by memory: the lookup by
-// the rows read and written, the gradient by the table written and dout read once.
+// the rows read and written, the gradient by the table written and dout read once (few tokens: by the latency of
+// its three launches).  MI355X, 32768 tokens of 50000 x 768 bf16: lookup 13.3 us (7.6 TB/s of rows, repeated ones from
+// cache), gradient 43.4 (count 5.5, place and zeros 18.5, pieces 17.8, join 5.2); 256 tokens of 2000 x 256: 4.2 and 11.4.
 #include "lbscan_device.h"
 #include "lbscan_embed.h"
 #include "lbscan_internal.h"

@@ -112,6 +112,14 @@ Tensor scratch(const Stream& stream, size_t bytes, const Tensor& like)
     return bytes ? fresh(stream, {(int64_t)bytes}, like, at::kByte) : Tensor();
 }
 
+// Gradients have no gradients of their own.  A backward pass that is itself recorded would leave them out of what
+// is differentiated next without a word, so it is refused.
+void refuse_second_derivatives()
+{
+    if (at::GradMode::is_enabled())
+        throw Failure(LBSCAN_EUNSUPPORTED, "lbscan operators can be differentiated once: backward with create_graph is not supported");
+}
+
 // ---- gated linear recurrence ---------------------------------------------------------------------------
 struct Gated {
     Tensor x, gate_a, gate_x, decay;
@@ -270,6 +278,7 @@ struct GatedNode : torch::autograd::Function<GatedNode> {
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads)
     {
+        refuse_second_derivatives();
         const auto s = ctx->get_saved_variables();
         Tensor dout = grads[0], dhT = grads.size() > 1 ? grads[1] : Tensor();
         variable_list r(10);
@@ -406,6 +415,7 @@ struct NormNode : torch::autograd::Function<NormNode> {
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads)
     {
+        refuse_second_derivatives();
         const auto s = ctx->get_saved_variables();
         Tensor dout = grads[0], dsum = grads.size() > 1 ? grads[1] : Tensor();
         variable_list r(5);
@@ -499,6 +509,7 @@ struct EmbedNode : torch::autograd::Function<EmbedNode> {
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads)
     {
+        refuse_second_derivatives();
         const Tensor dout = grads[0].contiguous();
         return {Tensor(), embed_gradient(ctx->get_saved_variables()[0], dout, ctx->saved_data["vocab"].toInt(),
                                          ctx->saved_data["scale"].toDouble(), Stream(dout)),

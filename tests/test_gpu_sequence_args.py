@@ -70,3 +70,19 @@ def test_embed(lb):
     refused(EUNSUPPORTED, lb.lbscan_embed_fwd, t(7, dtype=torch.int16), table)
     refused(EINVAL, lb.lbscan_embed_bwd, ids, dout=t(8, 7).t(), vocab=5)
     refused(EINVAL, lb.lbscan_embed_bwd, ids, dout=t(7, 8), vocab=0)
+
+
+def test_second_derivatives_are_refused(lb):
+    from paper_2506_15976_amd.autograd import gated_linear_recurrence, layer_norm, token_embedding
+    x = torch.randn(2, 3, 40, device="cuda", requires_grad=True)
+    decay = torch.zeros(3, device="cuda", requires_grad=True)
+    table = torch.randn(5, 8, device="cuda", requires_grad=True)
+    ids = torch.randint(0, 5, (7,), device="cuda")
+    res = torch.randn(2, 3, 40, device="cuda")
+    for f, leaf in ((lambda: gated_linear_recurrence(x, x, x, decay), x), (lambda: layer_norm(x), x),
+                    (lambda: layer_norm(x, residual=res)[0], x), (lambda: token_embedding(ids, table), table)):
+        y = f()
+        g, = torch.autograd.grad((y ** 2).sum(), leaf, retain_graph=True)
+        assert torch.isfinite(g).all()
+        with pytest.raises(RuntimeError, match="once"):
+            torch.autograd.grad((y ** 2).sum(), leaf, create_graph=True)
