@@ -166,7 +166,7 @@ def test_closed_and_open_gates(lb, L):
     close(g["ddecay"], want["ddecay"], GATED["fp32"], "ddecay")
 
 
-@pytest.mark.parametrize("decay", [-60.0, 0.0, 5.0, 40.0])
+@pytest.mark.parametrize("decay", [-60.0, -4.1, -3.3, -2.5, 0.0, 5.0, 40.0])
 def test_decay_range(lb, decay):
     t, more = make(2, 3, 100, seed=8)
     t["decay"][:] = decay
