@@ -374,12 +374,12 @@ __global__ __launch_bounds__(256) void embed_pieces_kernel(const EmbedParams p, 
 // The rows whose tokens lie in several pieces: the piece in which they begin finds them by its last token and
 // adds the others' sums, eight waves a share each, in a fixed order.
 template <typename T, int E>
-__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const EmbedParams p)
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const EmbedParams p, int first_piece)
 {
     __shared__ float sums[kJoinWaves - 1][64][E];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int dim = p.dim, packs = (dim + E - 1) / E;
-    const int piece = blockIdx.x, begins = piece * p.piece, last = begins + p.piece - 1, valid = *p.valid;
+    const int piece = first_piece + (int)blockIdx.x, begins = piece * p.piece, last = begins + p.piece - 1, valid = *p.valid;
     if (last + 1 >= valid) return;                                     // nothing behind this piece
     const int row = p.row[last];
     if (p.row[last + 1] != row) return;
@@ -423,14 +423,22 @@ int pieces_of(const EmbedParams& p)
 }
 
 template <typename T, int E>
-hipError_t launch_fwd(const EmbedParams& p, hipStream_t stream)
+hipError_t launch_fwd(EmbedParams p, hipStream_t stream)
 {
-    const long waves = (p.tokens + kLookup - 1) / kLookup;
     const int packs = (p.dim + E - 1) / E, tiles = (packs + 63) / 64;
-    const dim3 grid((unsigned)((waves + 3) / 4), tiles < 64 ? tiles : 64);
-    if (p.wide_ids) embed_fwd_kernel<T, int64_t, E><<<grid, 256, 0, stream>>>(p);
-    else embed_fwd_kernel<T, int32_t, E><<<grid, 256, 0, stream>>>(p);
-    return hipGetLastError();
+    constexpr int kTokens = 4 * kLookup;             // of a block
+    constexpr long most = most_blocks(256) * kTokens;
+    for (long left = p.tokens; left > 0; left -= most) {
+        p.tokens = left < most ? left : most;
+        const dim3 grid((unsigned)((p.tokens + kTokens - 1) / kTokens), tiles < 64 ? tiles : 64);
+        if (p.wide_ids) embed_fwd_kernel<T, int64_t, E><<<grid, 256, 0, stream>>>(p);
+        else embed_fwd_kernel<T, int32_t, E><<<grid, 256, 0, stream>>>(p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        p.ids = static_cast<const char*>(p.ids) + p.tokens * (p.wide_ids ? 8 : 4);
+        p.out = static_cast<T*>(p.out) + p.tokens * p.dim;
+    }
+    return hipSuccess;
 }
 
 template <typename T, int E>
@@ -439,12 +447,16 @@ hipError_t launch_sums(const EmbedParams& p, hipStream_t stream)
     const int pieces = pieces_of(p), packs = (p.dim + E - 1) / E, tiles = (packs + 63) / 64;
     const long tasks = (long)pieces * tiles;
     if (tasks == 0) return hipSuccess;
-    if (tasks > 0x7fffffffL) return hipErrorInvalidValue;
+    if ((tasks + 3) / 4 > most_blocks(256)) return hipErrorInvalidConfiguration;      // (a dout of a terabyte)
     embed_pieces_kernel<T, E><<<(unsigned)((tasks + 3) / 4), 256, 0, stream>>>(p, pieces, tiles);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || pieces < 2) return e;
-    embed_join_kernel<T, E><<<dim3(pieces - 1, tiles), 64 * kJoinWaves, 0, stream>>>(p);
-    return hipGetLastError();
+    constexpr long most = most_blocks(64 * kJoinWaves);
+    for (long first = 0; e == hipSuccess && first < pieces - 1; first += most) {
+        const long n = pieces - 1 - first < most ? pieces - 1 - first : most;
+        embed_join_kernel<T, E><<<dim3((unsigned)n, tiles), 64 * kJoinWaves, 0, stream>>>(p, (int)first);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 }  // namespace

@@ -11,6 +11,10 @@ namespace lbscan {
 // Keeps the text of a HIP error for lbscan_last_error(); LBSCAN_EHIP.
 int hip_fail(hipError_t e, const char* where);
 
+// Most blocks of one launch: the threads along an axis of its grid have to fit 32 bits.  A larger grid is no error, it
+// wraps: of 2^32 + n threads only n run.
+constexpr long most_blocks(int threads) { return 0xffffffffL / threads; }
+
 // Arguments of one forward launch, already validated by the C entry points.
 struct FwdParams {
     int batch, dim, dstate, seqlen;
