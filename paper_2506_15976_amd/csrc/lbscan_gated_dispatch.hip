@@ -8,10 +8,11 @@ namespace {
 // ddecay[d] = sigma(decay) / softplus(decay) * sum over batch entries and segments of the rows' sums, in a
 // fixed order.  16 channels a block, 16 threads to a channel.
 __global__ __launch_bounds__(256) void gated_decay_kernel(const float* __restrict__ qsum, const float* __restrict__ decay,
-                                                          float* __restrict__ ddecay, int dim, int shares)
+                                                          float* __restrict__ ddecay, unsigned first, unsigned dim, int shares)
 {
     __shared__ float part[16][17];
-    const int lane = threadIdx.x & 15, group = threadIdx.x >> 4, d = blockIdx.x * 16 + lane;
+    const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
+    const unsigned d = (first + blockIdx.x) * 16 + lane;
     float s = 0.0f, slope = 0.0f, soft = 1.0f, own = 0.0f;
     if (d < dim) {
         own = decay[d];
@@ -150,8 +151,14 @@ hipError_t launch_gated_bwd(GatedParams p, float* workspace, const float* saved,
     }
     if (p.nseg > 1 && (e = launch_kernels(p, GatedPass::backward_summary, stream)) != hipSuccess) return e;
     if ((e = launch_kernels(p, GatedPass::backward, stream)) != hipSuccess) return e;
-    gated_decay_kernel<<<(p.dim + 15) / 16, 256, 0, stream>>>(p.qsum, p.decay, p.ddecay, p.dim, p.nseg * p.batch);
-    return hipGetLastError();
+    const unsigned blocks = ((unsigned)p.dim + 15) / 16;
+    constexpr unsigned most = (unsigned)most_blocks(256);
+    for (unsigned first = 0; e == hipSuccess && first < blocks; first += most) {
+        gated_decay_kernel<<<blocks - first < most ? blocks - first : most, 256, 0, stream>>>(p.qsum, p.decay, p.ddecay, first,
+                                                                                              (unsigned)p.dim, p.nseg * p.batch);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 }  // namespace lbscan
