@@ -350,12 +350,13 @@ __global__ __launch_bounds__(kBwdThreads<W>) void norm_bwd_kernel(const NormPara
     }
 }
 
-// Rows too long for registers: a block a row, which reads it once for each of mean, deviation and result.
+// Rows too long for registers: a block a row, which reads it once for each of mean, deviation and result.  `first`: of the
+// launch, where the rows take several.
 template <typename T, bool RES>
-__global__ __launch_bounds__(1024) void norm_long_fwd_kernel(const NormParams p)
+__global__ __launch_bounds__(1024) void norm_long_fwd_kernel(const NormParams p, long first)
 {
     __shared__ float slots[2][16];
-    const long at = (long)blockIdx.x * p.dim;
+    const long row = first + blockIdx.x, at = row * p.dim;
     const T* x = static_cast<const T*>(p.x) + at;
     auto value = [&](int c) { return RES ? to_f32(x[c]) + p.residual[at + c] : to_f32(x[c]); };
     float sum = 0.0f;
@@ -371,21 +372,21 @@ __global__ __launch_bounds__(1024) void norm_long_fwd_kernel(const NormParams p)
         square += s * s;
     }
     const float rstd = 1.0f / sqrtf(team_sum<64, 16>(square, &slots[1]) / (float)p.dim + p.eps);
-    if (p.mean && threadIdx.x == 0) { p.mean[blockIdx.x] = mean; p.rstd[blockIdx.x] = rstd; }
+    if (p.mean && threadIdx.x == 0) { p.mean[row] = mean; p.rstd[row] = rstd; }
     for (int c = threadIdx.x; c < p.dim; c += 1024) {
         const float s = (RES ? p.sum[at + c] : value(c)) - mean;
         static_cast<T*>(p.y)[at + c] = from_f32<T>(fmaf(s * rstd, p.weight ? p.weight[c] : 1.0f, p.bias ? p.bias[c] : 0.0f));
     }
 }
 template <typename T, bool RES>
-__global__ __launch_bounds__(1024) void norm_long_bwd_kernel(const NormParams p)
+__global__ __launch_bounds__(1024) void norm_long_bwd_kernel(const NormParams p, long first)
 {
     using S = std::conditional_t<RES, float, T>;
     __shared__ float slots[2][16];
-    const long at = (long)blockIdx.x * p.dim;
+    const long row = first + blockIdx.x, at = row * p.dim;
     const S* s = (RES ? reinterpret_cast<const S*>(p.sum) : static_cast<const S*>(p.x)) + at;
     const T* dy = static_cast<const T*>(p.dy) + at;
-    const float mean = p.mean[blockIdx.x], rstd = p.rstd[blockIdx.x];
+    const float mean = p.mean[row], rstd = p.rstd[row];
     float sum_g = 0.0f, sum_gh = 0.0f;
     for (int c = threadIdx.x; c < p.dim; c += 1024) {
         const float g = to_f32(dy[c]) * (p.weight ? p.weight[c] : 1.0f);
@@ -511,13 +512,16 @@ hipError_t launch_typed(const NormParams& p, bool backward, hipStream_t stream)
 {
     const NormShape s = norm_shape(p);
     if (s.packs == 0) {
-        if (p.rows > 0x7fffffffL) return hipErrorInvalidValue;
-        if (!backward) {
-            norm_long_fwd_kernel<T, RES><<<(unsigned)p.rows, 1024, 0, stream>>>(p);
-        } else {
-            norm_long_bwd_kernel<T, RES><<<(unsigned)p.rows, 1024, 0, stream>>>(p);
-            if (p.dweight || p.dbias) norm_long_columns_kernel<T, RES><<<dim3((p.dim + 255) / 256, p.shares), 256, 0, stream>>>(p);
+        constexpr long most = most_blocks(1024);
+        for (long first = 0; first < p.rows; first += most) {
+            const unsigned n = (unsigned)(p.rows - first < most ? p.rows - first : most);
+            if (backward) norm_long_bwd_kernel<T, RES><<<n, 1024, 0, stream>>>(p, first);
+            else norm_long_fwd_kernel<T, RES><<<n, 1024, 0, stream>>>(p, first);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
         }
+        if (!backward || (!p.dweight && !p.dbias)) return hipSuccess;
+        norm_long_columns_kernel<T, RES><<<dim3((p.dim + 255) / 256, p.shares), 256, 0, stream>>>(p);
         return hipGetLastError();
     }
     const int per = norm_block_rows(s);
