@@ -12,7 +12,8 @@ def lb():
     assert torch.cuda.is_available(), "GPU tests need a GPU"
     import paper_2506_15976_amd as pkg
     pkg.load()
-    return pkg
+    yield pkg
+    torch.cuda.empty_cache()          # (the blocks are large)
 
 
 @pytest.mark.parametrize("kind", [torch.int32, torch.int64])
