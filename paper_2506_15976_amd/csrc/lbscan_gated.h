@@ -37,7 +37,6 @@ struct GatedParams {
     float* hT;                  // (B, D), nullable
     // Tiles of lanes * waves * gated_lane_tokens tokens, one team of lanes a row
     int lanes, waves;
-    unsigned first_block;       // of the launch, where the rows take several
     int ntiles;
     float* ckpt;                // (B * D, ntiles), nullable: state entering each tile
     // Rows cut into nseg segments of seg_tiles tiles, a team each
