@@ -12,18 +12,15 @@
 //     dgate_a = q (1 - r)    ddecay = sigma(decay) / softplus(decay) * sum of q
 // la / beta has the limit 0 where the gate closes (la -> 0, beta ~ sqrt(-2 la)): every gradient is finite.
 #pragma once
+#include "lbscan_gated_plan.h"
+
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
 
 namespace lbscan {
 
-// Tokens that a lane holds: 16 bytes of a row.
-constexpr int gated_lane_tokens(int dtype) { return dtype == 0 ? 4 : 8; }
-// Rows shorter than this are walked by one lane each.
-constexpr int kGatedShort = 8;
-
-struct GatedParams {
+struct GatedParams : GatedShape {
     int batch, dim, seqlen;
     int dtype, reverse;
     float rate;
@@ -35,13 +32,8 @@ struct GatedParams {
     const float* h0;            // (B, D), nullable: zeros
     void* y;                    // nullable: states are not wanted (checkpoint launch)
     float* hT;                  // (B, D), nullable
-    // Tiles of lanes * waves * gated_lane_tokens tokens, one team of lanes a row
-    int lanes, waves;
-    int ntiles;
     float* ckpt;                // (B * D, ntiles), nullable: state entering each tile
-    // Rows cut into nseg segments of seg_tiles tiles, a team each
-    int nseg, seg_tiles;
-    float* seg_prod;            // (nseg, B * D): product of a over the segment (-0: a sequence starts in it)
+    float* seg_prod;            // cut rows: (nseg, B * D): product of a over the segment (-0: a sequence starts in it)
     float* seg_state;           // (nseg, B * D): the state that it reaches from zero
     float* seg_psi;             // (nseg, B * D): the gradient that it passes on to the left from zero
     // backward
