@@ -8,6 +8,7 @@
 #include "../../include/lbscan.h"
 
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/StreamGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/extension.h>
 
@@ -79,37 +80,48 @@ Maybe maybe(const Tensor& t) { return t.defined() ? Maybe(t) : Maybe(); }
 Tensor tensor(const Maybe& t) { return t ? *t : Tensor(); }
 
 // ---- streams -----------------------------------------------------------------------------------------
-// The stream of a call: the current one of the tensors' device, or a torch.cuda.Stream that the caller names.
-// Memory that the call takes from the allocator (which thinks of the current stream) is tied to a named one.
+// The stream of a call: the current one of the tensors' device, or a torch.cuda.Stream that the caller names.  Memory
+// that the call takes is the named stream's: a block of the current stream's may have been freed with kernels that
+// use it still queued there, and the call does not wait for them.  Outputs are tied to the current stream, where the caller
+// goes on with them.
 struct Stream {
     void* raw;
-    std::optional<c10::Stream> named;
+    std::optional<c10::Stream> named, current;         // where they are different streams
     Stream(const py::object& s, const Tensor& like)
     {
-        if (s.is_none()) {
-            raw = like.is_cuda() ? c10::hip::getCurrentHIPStream(like.device().index()).stream() : nullptr;
-        } else {
-            raw = reinterpret_cast<void*>(s.attr("cuda_stream").cast<uintptr_t>());
-            named = c10::Stream::unpack3(s.attr("stream_id").cast<int64_t>(), s.attr("device_index").cast<c10::DeviceIndex>(),
-                                         static_cast<c10::DeviceType>(s.attr("device_type").cast<int>()));
+        raw = like.is_cuda() ? c10::hip::getCurrentHIPStream(like.device().index()).stream() : nullptr;
+        if (s.is_none() || !like.is_cuda()) return;
+        const auto device = s.attr("device_index").cast<c10::DeviceIndex>();
+        if (device != like.device().index())
+            throw Failure(LBSCAN_EINVAL, "stream: of device " + std::to_string(device) + ", the tensors are on device " +
+                                             std::to_string(like.device().index()));
+        raw = reinterpret_cast<void*>(s.attr("cuda_stream").cast<uintptr_t>());
+        const auto other = c10::Stream::unpack3(s.attr("stream_id").cast<int64_t>(), device, like.device().type());
+        const auto here = c10::impl::VirtualGuardImpl(like.device().type()).getStream(like.device());
+        if (other != here) {
+            named = other;
+            current = here;
         }
     }
     explicit Stream(const Tensor& like) : raw(c10::hip::getCurrentHIPStream(like.device().index()).stream()) {}
-    void tie(const Tensor& t) const
-    {
-        if (named && t.defined()) t.record_stream(*named);
-    }
 };
 
+// An output, or what goes on to another call.
 Tensor fresh(const Stream& stream, at::IntArrayRef shape, const Tensor& like, at::ScalarType type)
 {
+    if (!stream.named) return at::empty(shape, like.options().dtype(type));
+    const c10::StreamGuard guard(*stream.named);
     Tensor t = at::empty(shape, like.options().dtype(type));
-    stream.tie(t);
+    if (t.numel()) t.record_stream(*stream.current);
     return t;
 }
+// Memory that goes back with the call.
 Tensor scratch(const Stream& stream, size_t bytes, const Tensor& like)
 {
-    return bytes ? fresh(stream, {(int64_t)bytes}, like, at::kByte) : Tensor();
+    if (!bytes) return Tensor();
+    c10::OptionalStreamGuard guard;
+    if (stream.named) guard.reset_stream(*stream.named);
+    return at::empty({(int64_t)bytes}, like.options().dtype(at::kByte));
 }
 
 // Gradients have no gradients of their own.  A backward pass that is itself recorded would leave them out of what
@@ -169,7 +181,7 @@ void keep(lbscan_gated_args& a, const Maybe& saved, const Tensor& like)
     a.saved_state_bytes = saved->numel() * 4;
 }
 
-Maybe gated_saved(const Tensor& x, bool reverse)
+Maybe gated_saved(const Tensor& x, bool reverse, const Stream& stream)
 {
     expect_axes("x", x, 3);
     lbscan_gated_args a{};
@@ -178,8 +190,9 @@ Maybe gated_saved(const Tensor& x, bool reverse)
     a.reverse = reverse;
     const size_t need = lbscan_gated_workspace_bytes(&a, LBSCAN_WS_SAVED);
     if (!need) return {};
-    return at::empty({(int64_t)(need / 4)}, x.options().dtype(at::kFloat));
+    return fresh(stream, {(int64_t)(need / 4)}, x, at::kFloat);
 }
+Maybe gated_saved_state(Tensor x, bool reverse, py::object stream) { return gated_saved(x, reverse, Stream(stream, x)); }
 
 std::pair<Tensor, Tensor> gated_run(const Gated& g, const Maybe& out, const Maybe& saved, bool return_state, const Stream& stream)
 {
@@ -267,9 +280,10 @@ struct GatedNode : torch::autograd::Function<GatedNode> {
         if (starts) starts = starts->contiguous();
         if (h0) h0 = h0->contiguous();
         expect_axes("x", x, 3);
-        const Maybe saved = keep_states ? gated_saved(x, reverse) : Maybe();
         if (!x.is_cuda()) throw Failure(LBSCAN_EINVAL, "x must be a device tensor");
-        auto [y, hT] = gated_run({x, gate_a, gate_x, decay, starts, h0, rate, reverse}, {}, saved, return_state, Stream(x));
+        const Stream stream(x);
+        const Maybe saved = keep_states ? gated_saved(x, reverse, stream) : Maybe();
+        auto [y, hT] = gated_run({x, gate_a, gate_x, decay, starts, h0, rate, reverse}, {}, saved, return_state, stream);
         ctx->save_for_backward({x, gate_a, gate_x, decay, tensor(starts), tensor(h0), tensor(saved)});
         ctx->saved_data["rate"] = rate;
         ctx->saved_data["reverse"] = reverse;
@@ -533,7 +547,7 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m)
     m.def("gated_fwd", gated_fwd);
     m.def("gated_step", gated_step);
     m.def("gated_bwd", gated_bwd);
-    m.def("gated_saved", gated_saved);
+    m.def("gated_saved", gated_saved_state);
     m.def("gated", gated);
     m.def("norm_fwd", norm_fwd);
     m.def("norm_bwd", norm_bwd);

@@ -1,7 +1,12 @@
 """Operators of recurrent sequence models around the scan: gated linear recurrence, layer norm, token
 embedding.  Names and defaults only: arguments are checked and the calls made in csrc/lbscan_torch.cpp, and every
 value is computed by the HIP kernels behind include/lbscan.h, which defines what each call returns.
-Refused arguments raise binding.LbscanError."""
+Refused arguments raise binding.LbscanError.
+
+stream: a torch.cuda.Stream to run on instead of the current one.  The call does not wait for the current stream, so the
+caller sees to it that the inputs (and tensors given to be written) are ready on that stream, and that the outputs
+are before they are used on another.  Outputs and scratch are that stream's memory, and outputs are tied to the
+current one."""
 from __future__ import annotations
 
 import importlib.util
@@ -28,10 +33,10 @@ def load():
     return _ext
 
 
-def lbscan_gated_saved_state(x, *, reverse=False):
+def lbscan_gated_saved_state(x, *, reverse=False, stream=None):
     """Buffer for lbscan_gated_fwd(saved_state=...) / lbscan_gated_bwd(saved_state=...), or None when
-    these sizes do not use one."""
-    return (_ext or load()).gated_saved(x, reverse)
+    these sizes do not use one.  stream: that of the calls it is for."""
+    return (_ext or load()).gated_saved(x, reverse, stream)
 
 
 def lbscan_gated_fwd(x, gate_a, gate_x, decay, *, rate=8.0, starts=None, reverse=False, h0=None,
