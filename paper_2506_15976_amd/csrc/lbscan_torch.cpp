@@ -124,6 +124,19 @@ Tensor scratch(const Stream& stream, size_t bytes, const Tensor& like)
     return at::empty({(int64_t)bytes}, like.options().dtype(at::kByte));
 }
 
+// ---- tensors that a call overwrites --------------------------------------------------------------------
+// The caller's own (a state, `out`): autograd has to know, by the tensor's version, as a backward pass may still need
+// what was there; and there is no gradient of the old values.
+void expect_writable(const char* name, const Maybe& t)
+{
+    if (t && t->requires_grad() && at::GradMode::is_enabled())
+        throw Failure(LBSCAN_EINVAL, std::string(name) + " requires grad and cannot be overwritten");
+}
+void written(const Maybe& t)
+{
+    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 // Gradients have no gradients of their own.  A backward pass that is itself recorded would leave them out of what
 // is differentiated next without a word, so it is refused.
 void refuse_second_derivatives()
@@ -199,6 +212,7 @@ std::pair<Tensor, Tensor> gated_run(const Gated& g, const Maybe& out, const Mayb
     lbscan_gated_args a = g.args();
     c10::DeviceGuard guard(g.x.device());
     expect("out", out, g.x.sizes(), g.x.scalar_type(), g.x);
+    expect_writable("out", out);
     Tensor y = out ? *out : fresh(stream, g.x.sizes(), g.x, g.x.scalar_type()), hT;
     if (return_state) hT = fresh(stream, {g.x.size(0), g.x.size(1)}, g.x, at::kFloat);
     a.y = y.data_ptr();
@@ -209,6 +223,8 @@ std::pair<Tensor, Tensor> gated_run(const Gated& g, const Maybe& out, const Mayb
     a.workspace = address(ws);
     a.workspace_bytes = need;
     check(lbscan_gated_fwd(&a, stream.raw), "lbscan_gated_fwd");
+    written(out);
+    written(saved);
     return {y, hT};
 }
 
@@ -229,10 +245,14 @@ Tensor gated_step(Tensor x, Tensor gate_a, Tensor gate_x, Tensor decay, Tensor s
     c10::DeviceGuard guard(x.device());
     const Stream stream(stream_object, x);
     expect("out", out, x.sizes(), x.scalar_type(), x);
+    expect_writable("out", out);
+    expect_writable("state", state);
     Tensor y = out ? *out : fresh(stream, x.sizes(), x, x.scalar_type());
     a.y = y.data_ptr();
     a.hT = address<float>(state);                    // updated in place
     check(lbscan_gated_fwd(&a, stream.raw), "lbscan_gated_step");
+    written(out);
+    written(state);
     return y;
 }
 
@@ -342,6 +362,7 @@ NormResult norm_run(const Tensor& x, const Maybe& weight, const Maybe& bias, con
     c10::DeviceGuard guard(x.device());
     expect("residual", residual, x.sizes(), at::kFloat, x);
     expect("out", out, x.sizes(), x.scalar_type(), x);
+    expect_writable("out", out);
     NormResult r;
     r.y = out ? *out : fresh(stream, x.sizes(), x, x.scalar_type());
     if (residual) r.sum = fresh(stream, x.sizes(), x, at::kFloat);
@@ -357,6 +378,7 @@ NormResult norm_run(const Tensor& x, const Maybe& weight, const Maybe& bias, con
     a.mean = address<float>(r.mean);
     a.rstd = address<float>(r.rstd);
     check(lbscan_norm_fwd(&a, stream.raw), "lbscan_norm_fwd");
+    written(out);
     return r;
 }
 
@@ -477,10 +499,12 @@ Tensor embed_run(const Tensor& ids, const Tensor& weight, double scale, const Ma
     c10::SmallVector<int64_t, 6> shape(ids.sizes().begin(), ids.sizes().end());
     shape.push_back(weight.size(1));
     expect("out", out, shape, weight.scalar_type(), weight);
+    expect_writable("out", out);
     Tensor y = out ? *out : fresh(stream, shape, weight, weight.scalar_type());
     a.weight = weight.data_ptr();
     a.out = y.data_ptr();
     check(lbscan_embed_fwd(&a, stream.raw), "lbscan_embed_fwd");
+    written(out);
     return y;
 }
 

@@ -6,7 +6,10 @@ Refused arguments raise binding.LbscanError.
 stream: a torch.cuda.Stream to run on instead of the current one.  The call does not wait for the current stream, so the
 caller sees to it that the inputs (and tensors given to be written) are ready on that stream, and that the outputs
 are before they are used on another.  Outputs and scratch are that stream's memory, and outputs are tied to the
-current one."""
+current one.
+
+out, and the state of a single step, are overwritten as in-place operations overwrite: autograd sees it by their versions, and
+tensors that require gradients are refused while gradients are recorded."""
 from __future__ import annotations
 
 import importlib.util
