@@ -10,6 +10,7 @@
 #include <c10/core/DeviceGuard.h>
 #include <c10/core/StreamGuard.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/extension.h>
 
 #include <optional>
@@ -135,6 +136,29 @@ void expect_writable(const char* name, const Maybe& t)
 void written(const Maybe& t)
 {
     if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
+// The Python error of a failure is set (the GIL is held).
+void set_python_error(const Failure& e)
+{
+    const py::object type = py::module_::import("paper_2506_15976_amd.binding").attr("LbscanError");
+    PyErr_SetObject(type.ptr(), type(e.code, e.what()).ptr());
+}
+
+// A node's backward pass.  Its errors cross torch's threads, which hand Python errors on as they are and make a RuntimeError
+// of every other exception.
+template <typename F>
+variable_list backward_pass(const F& pass)
+{
+    try {
+        return pass();
+    } catch (const Failure& e) {
+        const py::gil_scoped_acquire gil;
+        set_python_error(e);
+        python_error error;
+        error.persist();
+        throw error;
+    }
 }
 
 // Gradients have no gradients of their own.  A backward pass that is itself recorded would leave them out of what
@@ -312,6 +336,10 @@ struct GatedNode : torch::autograd::Function<GatedNode> {
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads)
     {
+        return backward_pass([&] { return gradients(ctx, grads); });
+    }
+    static variable_list gradients(AutogradContext* ctx, const variable_list& grads)
+    {
         refuse_second_derivatives();
         const auto s = ctx->get_saved_variables();
         Tensor dout = grads[0], dhT = grads.size() > 1 ? grads[1] : Tensor();
@@ -451,6 +479,10 @@ struct NormNode : torch::autograd::Function<NormNode> {
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads)
     {
+        return backward_pass([&] { return gradients(ctx, grads); });
+    }
+    static variable_list gradients(AutogradContext* ctx, const variable_list& grads)
+    {
         refuse_second_derivatives();
         const auto s = ctx->get_saved_variables();
         Tensor dout = grads[0], dsum = grads.size() > 1 ? grads[1] : Tensor();
@@ -547,6 +579,10 @@ struct EmbedNode : torch::autograd::Function<EmbedNode> {
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads)
     {
+        return backward_pass([&] { return gradients(ctx, grads); });
+    }
+    static variable_list gradients(AutogradContext* ctx, const variable_list& grads)
+    {
         refuse_second_derivatives();
         const Tensor dout = grads[0].contiguous();
         return {Tensor(), embed_gradient(ctx->get_saved_variables()[0], dout, ctx->saved_data["vocab"].toInt(),
@@ -564,8 +600,7 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m)
         try {
             if (p) std::rethrow_exception(p);
         } catch (const Failure& e) {
-            const py::object type = py::module_::import("paper_2506_15976_amd.binding").attr("LbscanError");
-            PyErr_SetObject(type.ptr(), type(e.code, e.what()).ptr());
+            set_python_error(e);
         }
     });
     m.def("gated_fwd", gated_fwd);
