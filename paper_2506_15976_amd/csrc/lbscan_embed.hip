@@ -4,6 +4,7 @@
 // cache), gradient 43.4 (count 5.5, place and zeros 18.5, pieces 17.8, join 5.2); 256 tokens of 2000 x 256: 4.2 and 11.4.
 #include "lbscan_device.h"
 #include "lbscan_embed.h"
+#include "lbscan_embed_plan.h"
 #include "lbscan_internal.h"
 
 #include <type_traits>
@@ -162,8 +163,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedPar
     const long share = ((block_end - block_begin + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
     const long begin = min(block_begin + share * wave, block_end), end = min(begin + share, block_end);
     // A bit of `hits` stands for 2^span_log2 groups of 64 ids and says whether one is the block's.
-    int span_log2 = 0;
-    while ((share >> 6 >> span_log2) > 64) ++span_log2;
+    const int span_log2 = sort_span_log2(share >> 6);
     uint64_t hits = 0;
 
     // What the launch before left is on its way meanwhile.  A thread has the rows threadIdx.x and, of many,
