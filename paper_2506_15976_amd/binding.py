@@ -8,6 +8,7 @@ built, loading fails with an error that says how to build it.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import struct
 
@@ -303,35 +304,47 @@ def _optional_block(nbytes, device):
 
 
 def _workspace_for(args, which, like, stream=None):
-    """Scratch for one call.  It is allocated from torch's caching allocator on the
-    current stream; when the call runs on another stream the block is tied to that
-    stream as well, so that it is not handed out again while the kernels use it."""
+    """Scratch for one call, out of the memory of its stream."""
     import torch
     need = lbscan_workspace_bytes(args, which)
-    ws = None
-    if args.scan_order:
-        # the larger scratch of the reordered copies, when the device has it
-        more = lbscan_workspace_bytes(args, {WS_FWD: WS_FWD_ORDER, WS_BWD: WS_BWD_ORDER}[which])
-        if more > need:
-            ws = _optional_block(more, like.device)
+    # the larger scratch of the reordered copies, when the device has it
+    more = lbscan_workspace_bytes(args, {WS_FWD: WS_FWD_ORDER, WS_BWD: WS_BWD_ORDER}[which]) if args.scan_order else 0
+    if max(need, more) == 0:
+        return None
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _workspace_of(args, need, more, like)
+    return _workspace_of(args, need, more, like)
+
+
+def _workspace_of(args, need, more, like):
+    import torch
+    ws = _optional_block(more, like.device) if more > need else None
     if ws is None:
         if need == 0:
             return None
         ws = torch.empty((need + 3) // 4, dtype=torch.float32, device=like.device)
-    _tie_to_stream(stream, ws)
     args.workspace = ws.data_ptr()
     args.workspace_bytes = ws.numel() * 4
     return ws
 
 
-def _tie_to_stream(stream, *tensors):
-    """Tensors this binding allocated (current stream) and hands to kernels that run
-    on `stream`: record the use, so that the caching allocator waits for it."""
-    if stream is None:
-        return
-    for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
+def _new(stream, make, like, **k):
+    """make(like, **k) out of the memory of `stream`, tied to the current stream."""
+    import torch
+    here = torch.cuda.current_stream(like.device)
+    with torch.cuda.stream(stream):
+        t = make(like, **k)
+    if stream != here:
+        t.record_stream(here)
+    return t
+
+
+def _maker(stream, make):
+    """How a call on `stream` makes its outputs and scratch.  On a stream that the caller names they are that
+    stream's memory: a block of the current stream's may have been freed with kernels that use it still queued there,
+    and the call does not wait for them.  Outputs are tied to the current stream, where the caller goes on with them."""
+    return make if stream is None else functools.partial(_new, stream, make)
 
 
 def _check_like(name, t, like):
@@ -343,13 +356,13 @@ def _check_like(name, t, like):
                                   f"{tuple(like.shape)} and dtype {like.dtype}")
 
 
-def lbscan_saved_state(x, A, *, window):
+def lbscan_saved_state(x, A, *, window, stream=None):
     """Buffer for lbscan_fwd(saved_state=...) / lbscan_bwd(saved_state=...), or None
-    when these shapes do not use one."""
+    when these shapes do not use one.  stream: that of the calls it is for."""
     import torch
     a = LbscanArgs(x.shape[0], x.shape[1], A.shape[1], x.shape[2], int(window), _dtype_code(x))
     need = lbscan_workspace_bytes(a, WS_SAVED)
-    return torch.empty((need + 3) // 4, dtype=torch.float32, device=x.device) if need else None
+    return _maker(stream, torch.Tensor.new_empty)(x, size=((need + 3) // 4,), dtype=torch.float32) if need else None
 
 
 def lbscan_fwd(x, delta, A, Bm, Cm, Dskip=None, z=None, delta_bias=None, *, window,
@@ -359,15 +372,14 @@ def lbscan_fwd(x, delta, A, Bm, Cm, Dskip=None, z=None, delta_bias=None, *, wind
     h0 (B,D,N) fp32: forward state entering the call; with return_state the result
     is (out, hT), hT the state that leaves it."""
     import torch
-    y = torch.empty_like(x) if out is None else out
+    y = _maker(stream, torch.empty_like)(x) if out is None else out
     hT = None
     if return_state:
-        hT = torch.empty((x.shape[0], x.shape[1], A.shape[1]), dtype=torch.float32, device=x.device)
+        hT = _maker(stream, torch.Tensor.new_empty)(x, size=(x.shape[0], x.shape[1], A.shape[1]), dtype=torch.float32)
     a = make_args(x, delta, A, Bm, Cm, Dskip, z, delta_bias, window=window,
                   delta_softplus=delta_softplus, reverse=reverse, y=y, saved_state=saved_state,
                   h0=h0, hT=hT, grid=grid)
     ws = _workspace_for(a, WS_FWD, x, stream)
-    _tie_to_stream(stream, y if out is None else None, hT)
     _check(load().lbscan_fwd(ctypes.byref(a), _stream(stream)), "lbscan_fwd")
     del ws
     return (y, hT) if return_state else y
@@ -391,7 +403,7 @@ def lbscan_bidir_fwd(set_f: dict, set_b: dict, *, out=None, stream=None):
     x, delta, A, Bm, Cm and optional Dskip, z, delta_bias, delta_softplus; the
     gate is set_f['z']."""
     import torch
-    y = torch.empty_like(set_f["x"]) if out is None else out
+    y = _maker(stream, torch.empty_like)(set_f["x"]) if out is None else out
 
     def mk(s, yy):
         return make_args(s["x"], s["delta"], s["A"], s["Bm"], s["Cm"], s.get("Dskip"), s.get("z"),
@@ -399,7 +411,6 @@ def lbscan_bidir_fwd(set_f: dict, set_b: dict, *, out=None, stream=None):
                          delta_softplus=s.get("delta_softplus", True), y=yy)
     af, ab = mk(set_f, y), mk(set_b, None)
     ws = _workspace_for(af, WS_BIDIR, y, stream)
-    _tie_to_stream(stream, y if out is None else None)
     _check(load().lbscan_bidir_fwd(ctypes.byref(af), ctypes.byref(ab), _stream(stream)),
            "lbscan_bidir_fwd")
     del ws
@@ -418,16 +429,16 @@ def lbscan_bwd(x, delta, A, Bm, Cm, Dskip=None, z=None, delta_bias=None, *, dout
                   delta_softplus=delta_softplus, reverse=reverse, saved_state=saved_state, h0=h0,
                   grid=grid)
     _check_like("dout", dout, x)
+    empty_like = _maker(stream, torch.empty_like)
     g = dict(
-        dx=torch.empty_like(x), ddelta=torch.empty_like(x),
-        dz=torch.empty_like(x) if z is not None else None,
-        dBm=torch.empty_like(Bm), dCm=torch.empty_like(Cm),
-        dA=torch.empty_like(A),
-        dDskip=torch.empty_like(Dskip) if Dskip is not None else None,
-        ddelta_bias=torch.empty_like(delta_bias) if delta_bias is not None else None,
+        dx=empty_like(x), ddelta=empty_like(x),
+        dz=empty_like(x) if z is not None else None,
+        dBm=empty_like(Bm), dCm=empty_like(Cm),
+        dA=empty_like(A),
+        dDskip=empty_like(Dskip) if Dskip is not None else None,
+        ddelta_bias=empty_like(delta_bias) if delta_bias is not None else None,
     )
     ws = _workspace_for(a, WS_BWD, x, stream)
-    _tie_to_stream(stream, *g.values())
     if h0 is None and dhT is None:
         rc = load().lbscan_bwd(ctypes.byref(a), _ptr(dout), _ptr(g["dx"]), _ptr(g["ddelta"]),
                                _ptr(g["dz"]), _ptr(g["dBm"]), _ptr(g["dCm"]), _ptr(g["dA"]),
@@ -438,8 +449,7 @@ def lbscan_bwd(x, delta, A, Bm, Cm, Dskip=None, z=None, delta_bias=None, *, dout
         if dhT is not None and (tuple(dhT.shape) != shape or dhT.dtype != torch.float32
                                 or not dhT.is_cuda or not dhT.is_contiguous()):
             raise LbscanError(EINVAL, f"dhT must be a contiguous float32 device tensor of shape {shape}")
-        g["dh0"] = torch.empty(shape, dtype=torch.float32, device=x.device)
-        _tie_to_stream(stream, g["dh0"])
+        g["dh0"] = _maker(stream, torch.Tensor.new_empty)(x, size=shape, dtype=torch.float32)
         rc = load().lbscan_bwd_state(ctypes.byref(a), _ptr(dout), _ptr(dhT), _ptr(g["dx"]),
                                      _ptr(g["ddelta"]), _ptr(g["dz"]), _ptr(g["dBm"]), _ptr(g["dCm"]),
                                      _ptr(g["dA"]), _ptr(g["dDskip"]), _ptr(g["ddelta_bias"]),
@@ -470,8 +480,7 @@ def lbscan_conv1d_fwd(x, weight, bias=None, *, activation=True, reverse=False, o
     import torch
     if out is not None:
         _check_like("out", out, x)
-    y = torch.empty_like(x) if out is None else out
-    _tie_to_stream(stream, y if out is None else None)
+    y = _maker(stream, torch.empty_like)(x) if out is None else out
     a = _conv_args(x, weight, bias, activation, reverse, y)
     _check(load().lbscan_conv1d_fwd(ctypes.byref(a), _stream(stream)), "lbscan_conv1d_fwd")
     return y
@@ -482,9 +491,8 @@ def lbscan_conv1d_bwd(x, weight, bias=None, *, dy, activation=True, reverse=Fals
     import torch
     _check_like("dy", dy, x)
     a = _conv_args(x, weight, bias, activation, reverse)
-    g = dict(dx=torch.empty_like(x), dweight=torch.empty_like(weight),
-             dbias=torch.empty_like(bias) if bias is not None else None)
-    _tie_to_stream(stream, *g.values())
+    empty_like = _maker(stream, torch.empty_like)
+    g = dict(dx=empty_like(x), dweight=empty_like(weight), dbias=empty_like(bias) if bias is not None else None)
     rc = load().lbscan_conv1d_bwd(ctypes.byref(a), _ptr(dy), _ptr(g["dx"]), _ptr(g["dweight"]),
                                   _ptr(g["dbias"]), _stream(stream))
     _check(rc, "lbscan_conv1d_bwd")
