@@ -149,7 +149,7 @@ hipError_t launch_chains(const FwdParams& p, const Chains& chains, int count, hi
     const long rows = (long)p.batch * p.dim;
     const long blocks = (rows + 63) / 64 * p.dstate;
     if (blocks == 0) return hipSuccess;
-    if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
+    if (blocks / p.dstate > most_blocks(64 * kChainWaves)) return hipErrorInvalidConfiguration;
     const int waves = (p.nseg + kPerWave - 1) / kPerWave;
     hipLaunchKernelGGL(carry_chain_kernel, dim3((unsigned)(blocks / p.dstate), count, p.dstate), dim3(64 * (waves < kChainWaves ? waves : kChainWaves)),
                        0, stream, chains, p.dsum, p.A, (int)rows, p.dim, p.dstate, p.nseg);
@@ -161,6 +161,7 @@ hipError_t launch_chains(const FwdParams& p, const Chains& chains, int count, hi
 hipError_t launch_zero(float* dst, long n, hipStream_t stream)
 {
     if (n <= 0 || !dst) return hipSuccess;
+    if ((n + 255) / 256 > most_blocks(256)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(zero_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, dst, n);
     return hipGetLastError();
 }
@@ -173,7 +174,7 @@ hipError_t launch_zero_many(ZeroMany z, hipStream_t stream)
         blocks += (z.n[k] + 255) / 256;
     }
     if (blocks == 0) return hipSuccess;
-    if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
+    if (blocks > most_blocks(256)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(zero_many_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, z);
     return hipGetLastError();
 }
@@ -182,6 +183,7 @@ hipError_t launch_copy(float* dst, const float* src, long n, hipStream_t stream)
 {
     if (!src) return launch_zero(dst, n, stream);
     if (n <= 0 || !dst) return hipSuccess;
+    if ((n + 255) / 256 > most_blocks(256)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(copy_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, dst, src, n);
     return hipGetLastError();
 }

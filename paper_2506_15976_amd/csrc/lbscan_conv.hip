@@ -395,7 +395,7 @@ hipError_t launch_conv_krh(ConvParams p, bool bwd, hipStream_t s)
     const long per_wave = p.items_per_wave;
     const long waves = (long)p.dim * ((items + per_wave - 1) / per_wave);
     const long blocks = (waves + kConvWaves - 1) / kConvWaves;
-    if (blocks > 0x3fffffffL) return hipErrorInvalidConfiguration;     // wave ids fit 32 bits
+    if (blocks > most_blocks(64 * kConvWaves)) return hipErrorInvalidConfiguration;
     if (bwd)
         hipLaunchKernelGGL((conv1d_bwd_kernel<T, K, REV, HOW>), dim3((unsigned)blocks), dim3(64 * kConvWaves), 0, s, p);
     else

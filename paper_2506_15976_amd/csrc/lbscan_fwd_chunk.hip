@@ -369,7 +369,7 @@ template <typename T>
 hipError_t launch_chunk_t(const FwdParams& p, hipStream_t s)
 {
     const long nblocks = (long)((p.dim + kR - 1) / kR) * p.batch;
-    if (nblocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
+    if (nblocks > most_blocks(64 * kR)) return hipErrorInvalidConfiguration;
     dim3 grid((unsigned)nblocks), block(64 * kR);
 #define LBSCAN_LAUNCH_CHUNK(M)                                                                 \
     if (p.reverse) hipLaunchKernelGGL((chunk_fwd_kernel<T, M, true, T>), grid, block, 0, s, p);   \

@@ -146,7 +146,7 @@ hipError_t launch_reorder_t(ReorderMany m, int L, const TokenOrder& map, hipStre
         total += m.blocks[i];
     }
     if (total == 0) return hipSuccess;
-    if (total > 0x7fffffffL) return hipErrorInvalidConfiguration;
+    if (total > most_blocks(kReThreads)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((reorder_kernel<TS, TD, GATE>), dim3((unsigned)total), dim3(kReThreads), 0, s,
                        m, L, rpb, map);
     return hipGetLastError();
