@@ -398,6 +398,12 @@ NormResult norm_run(const Tensor& x, const Maybe& weight, const Maybe& bias, con
         const auto rows = x.sizes().slice(0, x.dim() - 1);
         r.mean = fresh(stream, rows, x, at::kFloat);
         r.rstd = fresh(stream, rows, x, at::kFloat);
+        if (x.size(-1) == 0) {                       // rows of no columns: no kernel runs
+            c10::OptionalStreamGuard on;
+            if (stream.named) on.reset_stream(*stream.named);
+            r.mean.zero_();
+            r.rstd.zero_();
+        }
     }
     a.x = x.data_ptr();
     a.residual = address<float>(residual);

@@ -68,7 +68,7 @@ def lbscan_norm_fwd(x, weight=None, bias=None, *, residual=None, eps=1e-5, retur
                     stream=None):
     """Layer norm over the last axis of x; weight, bias (dim) fp32.  With residual (fp32, x's shape) the
     sum x + residual is normalised and the result is (y, sum), the sum in fp32; with return_stats the means
-    and reciprocal deviations of the rows follow, for lbscan_norm_bwd."""
+    and reciprocal deviations of the rows follow, for lbscan_norm_bwd (zeros where rows have no columns)."""
     return (_ext or load()).norm_fwd(x, weight, bias, residual, eps, return_stats, out, stream)
 
 
