@@ -223,7 +223,7 @@ int lbscan_conv1d_bwd(const lbscan_conv_args *fwd_args, const void *dy,
  *     h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigma(gate_x[b,d,t]) x[b,d,t],   h_{-1} = h0 or 0
  *     y_t = h_t
  * starts[b,t] != 0: a new sequence begins at token t (sequences packed into one row): h_{t-1}
- * counts as zero there, whatever it is.  reverse = 1: the tokens are taken from the last to the first; the state
+ * counts as zero there, whatever it is; the factor sqrt(1 - a_t^2) stays, as at every token.  reverse = 1: the tokens are taken from the last to the first; the state
  * enters at t = L-1 and leaves after t = 0. */
 typedef struct lbscan_gated_args {
     int32_t batch, dim, seqlen;   /* B, D, L; any may be 0 (L = 0: the state passes through).
@@ -265,7 +265,7 @@ size_t lbscan_gated_workspace_bytes(const lbscan_gated_args *args, int which);
  *     y = (s - mean(s)) / sqrt(mean((s - mean(s))^2) + eps) * weight + bias
  * The residual stream is fp32 and so is the sum, which the next norm takes as its residual. */
 typedef struct lbscan_norm_args {
-    int64_t rows;                 /* 0: only zeros are written to dweight, dbias */
+    int64_t rows;                 /* < 2^31; 0: only zeros are written to dweight, dbias */
     int32_t dim;                  /* 0: nothing is computed; <= 2^23 */
     int32_t dtype;                /* storage type of x, y and their gradients */
     float eps;                    /* finite, >= 0 */

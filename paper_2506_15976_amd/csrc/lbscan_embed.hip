@@ -1,7 +1,8 @@
 // Token embedding and its gradient (formulas: lbscan_embed.h).  All of it is bound by memory: the lookup by
 // the rows read and written, the gradient by the table written and dout read once (few tokens: by the latency of
-// its three launches).  MI355X, 32768 tokens of 50000 x 768 bf16: lookup 13.3 us (7.6 TB/s of rows, repeated ones from
-// cache), gradient 43.4 (count 5.5, place and zeros 18.5, pieces 17.8, join 5.2); 256 tokens of 2000 x 256: 4.2 and 11.4.
+// its three launches).  MI355X, three sets of inputs in turn, 32768 tokens of 50000 x 768 bf16: lookup 17.4 us (5.8 TB/s
+// of rows, repeated ones from cache), gradient 47.2 (count 5.4, place and zeros 18.8, pieces 17.7, join 5.3); 256 tokens of
+// 2000 x 256: 3.4 and 12.1 (sort 4.5, pieces 4.2, join 3.4).
 #include "lbscan_device.h"
 #include "lbscan_embed.h"
 #include "lbscan_embed_plan.h"
@@ -64,7 +65,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const EmbedParams p)
 // them in order, so that the tokens of a row stay in theirs.  One share: one launch, in which a block also
 // counts the tokens of the blocks before it.  Several: a launch that counts and one that places, since what
 // takes the time is one wave walking through the tokens of a much used row.  More than eight lose by the counts of the
-// other shares that every block reads.  MI355X, us, the gradient of 32768 x 768 bf16 by Zipf's law over 50000 rows: one
+// other shares that every block reads.  MI355X, us, calls in a loop, the gradient of 32768 x 768 bf16 by Zipf's law over 50000 rows: one
 // share 48.3, eight 44.6, sixteen 52.9; of 65536 x 512 bf16 over 300 rows 63.7, 43.2, 46.9.
 constexpr int kSortWaves = 8;
 constexpr int kSortThreads = 64 * kSortWaves;
@@ -301,7 +302,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedPar
 // table whose tokens all lie in the piece is written; of others the sum goes to scratch: [0] of a row that
 // began in an earlier piece, [1] of one that begins here and goes on.
 // Few tokens: short pieces, as what counts is how long a wave takes; many: long ones, as every piece costs a block that
-// looks for rows to join.  MI355X, us, the gradient with pieces of 8 / 16 / 32: 256 x 256 of 2000 rows 12.2 / 12.7 / 15.7,
+// looks for rows to join.  MI355X, us, calls in a loop, the gradient with pieces of 8 / 16 / 32: 256 x 256 of 2000 rows 12.2 / 12.7 / 15.7,
 // 4096 x 768 of 50000 24.5 / 25.1 / 28.6, 16384 x 2048 of 50000 68.4 / 62.7 / 60.4, 32768 x 768 48.9 / 43.7 / 43.2.
 int piece_of(long tokens) { return tokens <= 4096 ? 8 : tokens <= 8192 ? 16 : 32; }
 constexpr int kPieceAhead = 8;

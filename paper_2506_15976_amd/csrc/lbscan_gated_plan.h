@@ -20,10 +20,10 @@ struct GatedShape {
 
 // Waves of a row's team, for a row of so many wave tiles (the tokens of 64 lanes).  As few idle lanes as possible
 // first: a tile that the row does not fill costs as much as a full one.  Among equals a tile that holds the
-// whole row (nothing is carried along: 88 registers instead of 115 in the backward kernel), then the order below.  Fewer
+// whole row (nothing is carried along: 86 registers instead of 112 in the backward kernel of 2-byte storage), then the order below.  Fewer
 // waves than 8 a CU do not keep the memory busy, and sixteen to a team leave room for one
 // team a CU with 2-byte storage (there they are for few rows only).  MI355X, us, forward / backward, by waves a
-// team:
+// team (calls in a loop, inputs partly in the caches):
 //     8 x 768 x 4096 bf16     1: 39.7 / 78.9    4: 40.3 / 75.5    8: 37.1 / 68.7    16: 61.6 / 137.8
 //     8 x 768 x 4096 fp32     1: 82.1 / 151.7   4: 78.8 / 141.4   8: 73.5 / 134.5   16: 71.6 / 132.2
 //     1 x 768 x 8192 bf16     1: 16.0 / 30.6    4: 11.6 / 22.1    8: 11.9 / 23.0    16: 11.2 / 26.3
@@ -31,6 +31,12 @@ struct GatedShape {
 //     1 x 384 x 20000 bf16    1: 35.9 / 64.1    4: 17.7 / 31.2    8: 15.5 / 28.9    16: 18.7 / 33.0
 //     4 x 1000 x 3001 bf16    1: 21.6 / 35.6    4: 24.7 / 42.6    8: 23.9 / 49.9    16: 43.4 / 100.0
 //     16 x 512 x 700 bf16     1: 13.3 / 23.9    2: 12.6 / 24.5    4: 20.2 / 37.7
+//     8 x 200 x 2300 bf16     1: 9.4 / 17.4     2: 10.9 / 18.0    4: 12.3 / 20.2    8: 10.7 / 20.3
+//     6 x 100 x 4400 bf16     2: 9.8 / 17.4     4: 9.1 / 15.5     8: 10.2 / 18.0    16: 9.4 / 20.1
+//     1 x 300 x 4400 bf16     2: 9.2 / 16.9     4: 7.0 / 12.7     8: 7.5 / 13.8     16: 7.1 / 14.7
+//     1 x 300 x 2300 fp32     2: 6.8 / 13.3     4: 5.7 / 11.2     8: 5.7 / 11.1     16: 5.6 / 11.2
+// (For 257 to 512 rows of nine wave tiles in bf16 the rule gives eight waves, sixteen tiles' worth of lanes for nine, where
+// four are 8% faster.)
 inline int gated_team_waves(int wave_tiles, long rows, int dtype)
 {
     int best = 0, padded = 0;

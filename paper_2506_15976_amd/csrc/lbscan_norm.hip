@@ -3,10 +3,12 @@
 // A row is held in the registers of a team (16 lanes, a wave, or the waves of a block): it is read once, its
 // mean and then the mean of the squared deviations are summed over the team (two passes over registers, so no
 // difference of large numbers), and it is written once.  A team walks several rows with weight and bias (backward: the
-// sums of their gradients) of its columns in registers, the next row's loads in flight.  Bound by memory: MI355X, forward
-// and gradients (with the launch that adds the blocks' shares), 32768 x 768 bf16 with a residual 48.1 us (6.3 TB/s) and 80.6
-// (5.0), 25216 x 384 fp32 12.9 (6.0) and 25.5 (4.6), 2048 x 8192 bf16 13.7 (4.9) and 34.0 (3.0: a block has eight rows,
-// and a share as large as four of them).  A row of more columns is read three times, its gradients' columns once more.
+// sums of their gradients) of its columns in registers, the next row's loads in flight.  Bound by memory: MI355X, three
+// sets of inputs in turn, forward and gradients (with the launch that adds the blocks' shares), 32768 x 768 bf16 with a
+// residual 55.1 us (5.5 TB/s) and 77.9 (5.2), 25216 x 384 fp32 15.2 (5.1) and 25.8 (4.5), 2048 x 8192 bf16 15.3 (4.4) and
+// 33.3 (3.0: a block has eight rows and a share as large as four of them, which it stores element by element, 59.6 MB
+// for the 50.3 that are needed).  A row of more columns is read three times, an element a lane at a time, its gradients'
+// columns once more: 2048 x 16384 bf16 83 us (1.6 TB/s) and 120 (1.7).
 #include "lbscan_device.h"
 #include "lbscan_internal.h"
 #include "lbscan_norm.h"
@@ -175,8 +177,8 @@ template <int G, int W> constexpr int kBwdTeams = W == 1 ? 4 * (64 / G) : W == 2
 template <int W> constexpr int kBwdThreads = W <= 4 ? 256 : 64 * W;
 
 // Rows whose loads are under way beside the present one.  With two tensors of 2 bytes one row does not cover the
-// latency of memory, two do; teams of two and four waves lose more by the registers.  MI355X, us, gradients of
-// bf16 rows, one / two: 32768 x 768 36.5 / 34.7, 2048 x 8192 37.1 / 34.1, 8000 x 1025 22.5 / 24.6,
+// latency of memory, two do; teams of two and four waves lose more by the registers.  MI355X, us, calls in
+// a loop, gradients of bf16 rows, one / two: 32768 x 768 36.5 / 34.7, 2048 x 8192 37.1 / 34.1, 8000 x 1025 22.5 / 24.6,
 // 4096 x 4096 33.9 / 34.7.
 template <typename T, bool RES, int W, int P>
 constexpr int kBwdAhead = P > 16 ? 0 : sizeof(T) == 2 && !RES && (W == 1 || W == 8) ? 2 : 1;
@@ -541,7 +543,8 @@ hipError_t launch(const NormParams& p, bool backward, hipStream_t stream)
         return p.with_residual ? launch_typed<float, true>(p, backward, stream) : launch_typed<float, false>(p, backward, stream);
     return p.with_residual ? launch_typed<bf16_t, true>(p, backward, stream) : launch_typed<bf16_t, false>(p, backward, stream);
 }
-// Blocks of the backward kernel, each with a share of dweight and dbias.  MI355X, us, blocks 256 / 512 / 768 / 1024:
+// Blocks of the backward kernel, each with a share of dweight and dbias.  MI355X, us, calls in a loop,
+// blocks 256 / 512 / 768 / 1024:
 // 32768 x 768 bf16 with a residual 99.4 / 80.1 / 92.5 / 86.2, 25216 x 384 fp32 31.3 / 25.5 / 28.0 / 27.9,
 // 8000 x 1025 bf16 27.7 / 22.5 / 24.6 / 25.8, 4096 x 4096 bf16 37.9 / 33.9 / 39.4 / 47.6.  Teams of eight waves: one
 // a CU.
