@@ -177,9 +177,12 @@ template <int G, int W> constexpr int kBwdTeams = W == 1 ? 4 * (64 / G) : W == 2
 template <int W> constexpr int kBwdThreads = W <= 4 ? 256 : 64 * W;
 
 // Rows whose loads are under way beside the present one.  With two tensors of 2 bytes one row does not cover the
-// latency of memory, two do; teams of two and four waves lose more by the registers.  MI355X, us, calls in
-// a loop, gradients of bf16 rows, one / two: 32768 x 768 36.5 / 34.7, 2048 x 8192 37.1 / 34.1, 8000 x 1025 22.5 / 24.6,
-// 4096 x 4096 33.9 / 34.7.
+// latency of memory, two do; teams of two and four waves lose more by the registers.  MI355X, us, calls in a loop, gradients
+// of 25 million values in bf16 by columns, one / two:
+//     a wave        200: 67.7 / 58.7   768: 37.2 / 35.2    1000: 33.5 / 35.5
+//     two waves     1025: 53.1 / 59.1  1500: 35.9 / 42.7   2000: 35.4 / 38.4
+//     four waves    2100: 51.3 / 52.4  4000: 41.6 / 42.2   4096: 42.3 / 43.1
+//     eight waves   4200: 56.5 / 44.9  6000: 47.2 / 39.6   8192: 46.8 / 41.5
 template <typename T, bool RES, int W, int P>
 constexpr int kBwdAhead = P > 16 ? 0 : sizeof(T) == 2 && !RES && (W == 1 || W == 8) ? 2 : 1;
 
