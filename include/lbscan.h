@@ -315,6 +315,105 @@ int lbscan_embed_bwd(const lbscan_embed_args *fwd_args, const void *dout, void *
                      void *hip_stream);
 size_t lbscan_embed_workspace_bytes(const lbscan_embed_args *args);
 
+/* ---- State space language models: serving, the norms around a block -----------------
+ * As above: storage types, ownership, streams and errors, sums in fp32 and in a fixed order. */
+
+/* One token of every sequence through the scan (window 1: a single token has no local backward part) and, with
+ * conv_width, through the convolution in front of it (lbscan_conv1d_fwd's, of x alone):
+ *     x' = SiLU?(conv_bias + sum_{k<K-1} conv_weight[d,k] conv_state[s,d,k] + conv_weight[d,K-1] x),   K = conv_width
+ *     dt = softplus?(delta + delta_bias)       state[s,d,n] = exp(dt A[d,n]) state[s,d,n] + dt Bm[b,n] x'
+ *     y = (sum_n Cm[b,n] state[s,d,n] + Dskip x') SiLU?(z)
+ * Both states are updated in place; conv_state holds the last K-1 inputs, oldest first.  Row b has the states at
+ * s = slots[b] of the pools, or at b without slots.  A row whose slot is outside [0, pool), or that an earlier row has already, is
+ * padding: its y is zeros and no state is touched for it. */
+typedef struct lbscan_step_args {
+    int32_t batch, dim, dstate;   /* B, D, N in 1 .. LBSCAN_MAX_DSTATE; B or D may be 0.  B * D < 2^31;
+                                     B <= 65536 with slots */
+    int32_t pool;                 /* rows of the states; >= B without slots */
+    int32_t dtype;                /* storage type of x, delta, z, Bm, Cm, conv_state, y */
+    int32_t delta_softplus;       /* 0/1 */
+    int32_t conv_width;           /* K, 1..4; 0: x goes into the scan as it is */
+    int32_t conv_activation;      /* 1: SiLU, 0: none */
+    /* elements from one row to the next of x, delta, z (>= D) and Bm, Cm (>= N), columns of wider
+       tensors as they may be; 0: dense */
+    int64_t x_stride, delta_stride, z_stride, b_stride, c_stride;
+    const void    *x;             /* (B,D) */
+    const void    *delta;         /* (B,D) raw */
+    const void    *Bm, *Cm;       /* (B,N) */
+    const void    *z;             /* (B,D) or NULL: no gate */
+    const float   *A;             /* (D,N) */
+    const float   *Dskip;         /* (D) or NULL: 0 */
+    const float   *delta_bias;    /* (D) or NULL: 0 */
+    const float   *conv_weight;   /* (D,K) */
+    const float   *conv_bias;     /* (D) or NULL: 0 */
+    void          *conv_state;    /* (pool,D,K-1); NULL for K <= 1 */
+    const int32_t *slots;         /* (B) or NULL */
+    float         *state;         /* (pool,D,N) */
+    void          *y;             /* (B,D) out */
+} lbscan_step_args;
+
+int lbscan_step(const lbscan_step_args *args, void *hip_stream);
+
+/* lbscan_conv1d_fwd for sequences that come in pieces (a prompt, its parts, single tokens with seqlen 1): the K-1 tokens
+ * before the piece are taken from the state, which is updated in place and holds the last K-1 inputs, oldest first.
+ * lengths[b], held to 0 .. L: tokens of row b that are there (a padded batch); y is zero behind them and x is not read, and the
+ * state leaves as it is after the last of them.  slots and pool as in lbscan_step; a row of padding has zeros in y. */
+typedef struct lbscan_conv_state_args {
+    int32_t batch, dim, seqlen;   /* B, D, L; any may be 0 (the state stays).  D * L < 2^31; B <= 65536 with slots */
+    int32_t width;                /* K, 1..4 */
+    int32_t pool;                 /* rows of the state; >= B without slots */
+    int32_t dtype;                /* storage type of x, state, y */
+    int32_t activation;           /* 1: SiLU, 0: none */
+    int64_t x_stride;             /* elements from one row b of x to the next, >= D * L; 0: dense */
+    const void    *x;             /* (B,D,L) */
+    const float   *weight;        /* (D,K) */
+    const float   *bias;          /* (D) or NULL: 0 */
+    void          *state;         /* (pool,D,K-1); NULL for K = 1 */
+    const int32_t *slots;         /* (B) or NULL */
+    const int32_t *lengths;       /* (B) or NULL: L */
+    void          *y;             /* (B,D,L) out */
+} lbscan_conv_state_args;
+
+int lbscan_conv1d_prompt(const lbscan_conv_state_args *args, void *hip_stream);
+
+/* The norms around a block (root mean square, no mean subtracted), with the block's gate and its residual stream, over
+ * the rows of (rows, dim):
+ *     v = x SiLU(gate)                                   (x without a gate)
+ *     u = v / sqrt(mean(v^2) + eps) * branch_weight       (norm_branch; else v * branch_weight)
+ *     s = residual_scale residual + u                     (u without a residual)
+ *     y = s / sqrt(mean(s^2) + eps) * weight              (norm_stream; else s)
+ * The residual stream is fp32 and so is the sum s, which the next block takes as its residual. */
+typedef struct lbscan_block_norm_args {
+    int64_t rows;                 /* < 2^31; 0: only zeros are written to dweight, dbranch */
+    int32_t dim;                  /* 0: nothing is computed; <= 2^23 */
+    int32_t dtype;                /* storage type of x, gate, y and their gradients */
+    int32_t norm_branch, norm_stream;   /* 0/1 */
+    float eps;                    /* finite, >= 0 */
+    float residual_scale;         /* not NaN */
+    const void  *x;               /* (rows, dim) */
+    const void  *gate;            /* (rows, dim) or NULL */
+    const float *residual;        /* (rows, dim) or NULL.  Backward: only whether there is one */
+    const float *branch_weight;   /* (dim) or NULL: ones */
+    const float *weight;          /* (dim) or NULL: ones.  NULL without norm_stream */
+    void        *y;               /* (rows, dim) out.  Not read by the backward call */
+    float       *sum;             /* (rows, dim), with a residual: out of the forward call (may be residual
+                                     itself), read by the backward call with norm_stream */
+    float       *branch_rstd, *stream_rstd;   /* (rows) out of the forward call, NULL: not wanted; read by the
+                                     backward call where there is the norm */
+    void        *workspace;       /* backward: lbscan_block_norm_workspace_bytes() */
+    size_t       workspace_bytes;
+} lbscan_block_norm_args;
+
+int lbscan_block_norm_fwd(const lbscan_block_norm_args *args, void *hip_stream);
+
+/* Gradients of lbscan_block_norm_fwd.  dout is the gradient of y, dsum (fp32, nullable, with a residual only) that of
+ * sum.  dx; dgate with a gate; dresidual (fp32) with a residual, may be NULL; dweight (norm_stream only) and dbranch (dim) may
+ * each be NULL: not wanted. */
+int lbscan_block_norm_bwd(const lbscan_block_norm_args *fwd_args, const void *dout, const float *dsum,
+                          void *dx, void *dgate, float *dresidual, float *dweight, float *dbranch, void *hip_stream);
+
+size_t lbscan_block_norm_workspace_bytes(const lbscan_block_norm_args *args);
+
 /* Bytes of device scratch the call named by `which` (LBSCAN_WS_*) needs for
  * these sizes; 0 means workspace may be NULL. */
 size_t lbscan_workspace_bytes(const lbscan_args *args, int which);

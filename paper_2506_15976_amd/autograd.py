@@ -100,3 +100,10 @@ def token_embedding(ids, weight, *, scale=1.0):
     """Differentiable scale * weight[ids]: ids int32 or int64 of any shape, weight (vocab, dim); zeros (and no
     gradient) for ids that are no row of the table."""
     return sequence.load().embed(ids, weight, scale)
+
+
+def block_norm(x, weight=None, *, gate=None, branch_weight=None, residual=None, residual_scale=1.0, norm_branch=False,
+               norm_stream=True, eps=1e-5):
+    """Differentiable norms around a block, with its gate and its residual stream (see lbscan_block_norm_fwd): returns
+    y, or (y, sum) with a residual, the sum in fp32."""
+    return sequence.load().block_norm(x, weight, gate, branch_weight, residual, residual_scale, norm_branch, norm_stream, eps)

@@ -27,6 +27,8 @@ EXPORTS = (
     "lbscan_gated_fwd", "lbscan_gated_bwd", "lbscan_gated_workspace_bytes",
     "lbscan_norm_fwd", "lbscan_norm_bwd", "lbscan_norm_workspace_bytes",
     "lbscan_embed_fwd", "lbscan_embed_bwd", "lbscan_embed_workspace_bytes",
+    "lbscan_step", "lbscan_conv1d_prompt",
+    "lbscan_block_norm_fwd", "lbscan_block_norm_bwd", "lbscan_block_norm_workspace_bytes",
 )
 
 
@@ -92,6 +94,34 @@ class LbscanEmbedArgs(ctypes.Structure):
     ]
 
 
+class LbscanStepArgs(ctypes.Structure):
+    """Mirror of struct lbscan_step_args."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("batch", "dim", "dstate", "pool", "dtype", "delta_softplus", "conv_width",
+                                                    "conv_activation")]
+    _fields_ += [(name, ctypes.c_int64) for name in ("x_stride", "delta_stride", "z_stride", "b_stride", "c_stride")]
+    _fields_ += [(name, ctypes.c_void_p) for name in ("x", "delta", "Bm", "Cm", "z", "A", "Dskip", "delta_bias", "conv_weight",
+                                                      "conv_bias", "conv_state", "slots", "state", "y")]
+
+
+class LbscanConvStateArgs(ctypes.Structure):
+    """Mirror of struct lbscan_conv_state_args."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("batch", "dim", "seqlen", "width", "pool", "dtype", "activation")]
+    _fields_ += [("x_stride", ctypes.c_int64)]
+    _fields_ += [(name, ctypes.c_void_p) for name in ("x", "weight", "bias", "state", "slots", "lengths", "y")]
+
+
+class LbscanBlockNormArgs(ctypes.Structure):
+    """Mirror of struct lbscan_block_norm_args."""
+    _fields_ = [
+        ("rows", ctypes.c_int64), ("dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("norm_branch", ctypes.c_int32),
+        ("norm_stream", ctypes.c_int32), ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
+        ("x", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("residual", ctypes.c_void_p),
+        ("branch_weight", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("y", ctypes.c_void_p), ("sum", ctypes.c_void_p),
+        ("branch_rstd", ctypes.c_void_p), ("stream_rstd", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
 class LbscanError(RuntimeError):
     def __init__(self, code: int, what: str):
         self.code = code
@@ -130,8 +160,12 @@ def load():
     lib.lbscan_conv1d_fwd.argtypes = [cp, vp]
     lib.lbscan_conv1d_bwd.restype = ctypes.c_int
     lib.lbscan_conv1d_bwd.argtypes = [cp] + [vp] * 5
+    for name, struct_type in (("step", LbscanStepArgs), ("conv1d_prompt", LbscanConvStateArgs)):
+        call = getattr(lib, f"lbscan_{name}")
+        call.restype = ctypes.c_int
+        call.argtypes = [ctypes.POINTER(struct_type), vp]
     for name, struct_type, tensors in (("gated", LbscanGatedArgs, 7), ("norm", LbscanNormArgs, 6),
-                                       ("embed", LbscanEmbedArgs, 2)):
+                                       ("embed", LbscanEmbedArgs, 2), ("block_norm", LbscanBlockNormArgs, 7)):
         sp = ctypes.POINTER(struct_type)
         fwd, bwd, size = (getattr(lib, f"lbscan_{name}_{what}") for what in ("fwd", "bwd", "workspace_bytes"))
         fwd.restype = bwd.restype = ctypes.c_int

@@ -37,5 +37,7 @@ struct NormParams {
 hipError_t launch_norm_fwd(const NormParams& p, hipStream_t stream);
 hipError_t launch_norm_bwd(NormParams p, float* workspace, hipStream_t stream);
 size_t norm_bwd_floats(const NormParams& p);
+// first, second (dim), nullable = the sums of part (shares, 2, dim) over the shares, in a fixed order.
+hipError_t launch_norm_reduce(const float* part, float* first, float* second, int dim, int shares, hipStream_t stream);
 
 }  // namespace lbscan

@@ -564,6 +564,12 @@ int norm_shares(const NormParams& p)
 
 size_t norm_bwd_floats(const NormParams& p) { return p.rows > 0 ? (size_t)norm_shares(p) * 2 * p.dim : 0; }
 
+hipError_t launch_norm_reduce(const float* part, float* first, float* second, int dim, int shares, hipStream_t stream)
+{
+    norm_reduce_kernel<<<(unsigned)((2 * (long)dim + 63) / 64), 1024, 0, stream>>>(part, first, second, dim, shares);
+    return hipGetLastError();
+}
+
 hipError_t launch_norm_fwd(const NormParams& p, hipStream_t stream) { return launch(p, false, stream); }
 
 hipError_t launch_norm_bwd(NormParams p, float* workspace, hipStream_t stream)
@@ -572,8 +578,7 @@ hipError_t launch_norm_bwd(NormParams p, float* workspace, hipStream_t stream)
     p.shares = norm_shares(p);
     hipError_t e = launch(p, true, stream);
     if (e != hipSuccess || (!p.dweight && !p.dbias)) return e;
-    norm_reduce_kernel<<<(unsigned)((2 * (long)p.dim + 63) / 64), 1024, 0, stream>>>(workspace, p.dweight, p.dbias, p.dim, p.shares);
-    return hipGetLastError();
+    return launch_norm_reduce(workspace, p.dweight, p.dbias, p.dim, p.shares, stream);
 }
 
 }  // namespace lbscan

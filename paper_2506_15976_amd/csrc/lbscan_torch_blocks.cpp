@@ -1,0 +1,336 @@
+// The operators of state space language models for torch (single steps and prompts, norms around a block): argument
+// checks, outputs and scratch, autograd nodes.  No arithmetic: every value is computed by the kernels behind include/lbscan.h.
+#include "lbscan_torch.h"
+
+namespace lbscan_torch {
+namespace {
+
+// A (B, n) tensor that may be columns of a wider one; its rows' distance.
+int64_t expect_rows(const char* name, const Tensor& t, int64_t B, int64_t n, at::ScalarType type, const Tensor& like)
+{
+    if (t.dim() != 2 || t.size(0) != B || t.size(1) != n || t.scalar_type() != type)
+        throw Failure(LBSCAN_EINVAL, std::string(name) + ": expected " + shape_of({B, n}) + " " + c10::toString(type) + ", got " +
+                                         shape_of(t.sizes()) + " " + c10::toString(t.scalar_type()));
+    const bool dense = t.is_contiguous();
+    if (!t.is_cuda() || t.device() != like.device() || !(dense || ((n <= 1 || t.stride(1) == 1) && (B <= 1 || t.stride(0) >= n))))
+        throw Failure(LBSCAN_EINVAL, std::string(name) + " must be a device tensor with contiguous rows, on the device of the others");
+    return dense || B <= 1 ? 0 : t.stride(0);
+}
+
+// An output of the caller's must not be one of the inputs.
+void expect_apart(const Maybe& out, const Maybe& input, const char* name)
+{
+    if (out && input && out->numel() && out->data_ptr() == input->data_ptr())
+        throw Failure(LBSCAN_EINVAL, std::string("out must not be ") + name);
+}
+
+// A pool of states, and the rows' places in it.
+int32_t expect_pool(const char* name, const Tensor& state, at::IntArrayRef rest, at::ScalarType type, const Maybe& slots, int64_t B,
+                    const Tensor& like)
+{
+    const int64_t S = state.dim() ? state.size(0) : -1;
+    c10::SmallVector<int64_t, 3> shape{S};
+    shape.append(rest.begin(), rest.end());
+    expect(name, state, shape, type, like);
+    expect("slots", slots, {B}, at::kInt, like);
+    if (!slots && S != B)
+        throw Failure(LBSCAN_EINVAL, std::string(name) + ": expected " + std::to_string(B) + " rows (one for each row of x, without slots), got " +
+                                         std::to_string(S));
+    expect_writable(name, state);
+    return size32(name, S);
+}
+
+// ---- single tokens through the scan ------------------------------------------------------------------------
+Tensor step(Tensor x, Tensor delta, Tensor A, Tensor Bm, Tensor Cm, Tensor state, Maybe Dskip, Maybe z, Maybe delta_bias, bool softplus,
+            Maybe conv_state, Maybe conv_weight, Maybe conv_bias, bool activation, Maybe slots, Maybe out, py::object stream_object)
+{
+    expect_axes("x", x, 2);
+    expect_axes("A", A, 2);
+    const int64_t B = x.size(0), D = x.size(1), N = A.size(1);
+    const auto type = x.scalar_type();
+    lbscan_step_args a{};
+    a.dtype = type_code("x", type);
+    a.x_stride = expect_rows("x", x, B, D, type, x);
+    a.delta_stride = expect_rows("delta", delta, B, D, type, x);
+    if (z) a.z_stride = expect_rows("z", *z, B, D, type, x);
+    a.b_stride = expect_rows("Bm", Bm, B, N, type, x);
+    a.c_stride = expect_rows("Cm", Cm, B, N, type, x);
+    expect("A", A, {D, N}, at::kFloat, x);
+    expect("Dskip", Dskip, {D}, at::kFloat, x);
+    expect("delta_bias", delta_bias, {D}, at::kFloat, x);
+    a.pool = expect_pool("state", state, {D, N}, at::kFloat, slots, B, x);
+    if (conv_weight) {
+        expect_axes("conv_weight", *conv_weight, 2);
+        const int64_t K = conv_weight->size(1);
+        expect("conv_weight", *conv_weight, {D, K}, at::kFloat, x);
+        expect("conv_bias", conv_bias, {D}, at::kFloat, x);
+        if (K < 1 || K > 4) throw Failure(LBSCAN_EUNSUPPORTED, "conv_weight: width " + std::to_string(K) + ", supported are 1 to 4");
+        if (!conv_state) throw Failure(LBSCAN_EINVAL, "conv_weight needs a conv_state");
+        if (expect_pool("conv_state", *conv_state, {D, K - 1}, type, slots, B, x) != a.pool)
+            throw Failure(LBSCAN_EINVAL, "conv_state: expected as many rows as state, " + std::to_string(a.pool));
+        a.conv_width = (int32_t)K;
+    } else if (conv_state || conv_bias) {
+        throw Failure(LBSCAN_EINVAL, "conv_state and conv_bias need a conv_weight");
+    }
+    c10::DeviceGuard guard(x.device());
+    const Stream stream(stream_object, x);
+    expect("out", out, {B, D}, type, x);
+    expect_writable("out", out);
+    expect_apart(out, x, "x");
+    expect_apart(out, delta, "delta");
+    expect_apart(out, z, "z");
+    Tensor y = out ? *out : fresh(stream, {B, D}, x, type);
+    a.batch = size32("x", B);
+    a.dim = size32("x", D);
+    a.dstate = size32("A", N);
+    a.delta_softplus = softplus;
+    a.conv_activation = activation;
+    a.x = x.data_ptr(); a.delta = delta.data_ptr(); a.Bm = Bm.data_ptr(); a.Cm = Cm.data_ptr();
+    a.z = address(z);
+    a.A = address<float>(A);
+    a.Dskip = address<float>(Dskip);
+    a.delta_bias = address<float>(delta_bias);
+    a.conv_weight = address<float>(conv_weight);
+    a.conv_bias = address<float>(conv_bias);
+    a.conv_state = address(conv_state);
+    a.slots = address<int32_t>(slots);
+    a.state = address<float>(state);
+    a.y = y.data_ptr();
+    check(lbscan_step(&a, stream.raw), "lbscan_step");
+    written(out);
+    written(state);
+    written(conv_state);
+    return y;
+}
+
+// x (B,D,L), or (B,D) for a single token.
+Tensor conv1d_prompt(Tensor x, Maybe state, Tensor weight, Maybe bias, bool activation, Maybe lengths, Maybe slots, Maybe out,
+                     bool single, py::object stream_object)
+{
+    const char* name = single ? "lbscan_conv1d_step" : "lbscan_conv1d_prompt";
+    expect_axes("x", x, single ? 2 : 3);
+    expect_axes("weight", weight, 2);
+    const int64_t B = x.size(0), D = x.size(1), L = single ? 1 : x.size(2), K = weight.size(1);
+    const auto type = x.scalar_type();
+    lbscan_conv_state_args a{};
+    a.dtype = type_code("x", type);
+    if (K < 1 || K > 4) throw Failure(LBSCAN_EUNSUPPORTED, "weight: width " + std::to_string(K) + ", supported are 1 to 4");
+    if (single) a.x_stride = expect_rows("x", x, B, D, type, x);
+    else expect("x", x, x.sizes(), type, x);
+    expect("weight", weight, {D, K}, at::kFloat, x);
+    expect("bias", bias, {D}, at::kFloat, x);
+    expect("lengths", lengths, {B}, at::kInt, x);
+    if (!state) throw Failure(LBSCAN_EINVAL, "state is missing");
+    a.pool = expect_pool("state", *state, {D, K - 1}, type, slots, B, x);
+    c10::DeviceGuard guard(x.device());
+    const Stream stream(stream_object, x);
+    expect("out", out, x.sizes(), type, x);
+    expect_writable("out", out);
+    expect_apart(out, x, "x");
+    Tensor y = out ? *out : fresh(stream, x.sizes(), x, type);
+    a.batch = size32("x", B);
+    a.dim = size32("x", D);
+    a.seqlen = size32("x", L);
+    a.width = (int32_t)K;
+    a.activation = activation;
+    a.x = x.data_ptr();
+    a.weight = address<float>(weight);
+    a.bias = address<float>(bias);
+    a.state = address(state);
+    a.slots = address<int32_t>(slots);
+    a.lengths = address<int32_t>(lengths);
+    a.y = y.data_ptr();
+    check(lbscan_conv1d_prompt(&a, stream.raw), name);
+    written(out);
+    written(state);
+    return y;
+}
+
+// ---- norms around a block ------------------------------------------------------------------------------------
+struct BlockNorm {
+    Tensor x;
+    Maybe weight, gate, branch_weight, residual;
+    double residual_scale;
+    bool norm_branch, norm_stream;
+    double eps;
+
+    lbscan_block_norm_args args() const
+    {
+        lbscan_block_norm_args a{};
+        if (x.dim() < 1) throw Failure(LBSCAN_EINVAL, "x needs an axis to normalise");
+        a.dtype = type_code("x", x.scalar_type());
+        const int64_t D = x.size(-1);
+        expect("x", x, x.sizes(), x.scalar_type(), x);
+        expect("gate", gate, x.sizes(), x.scalar_type(), x);
+        expect("residual", residual, x.sizes(), at::kFloat, x);
+        expect("weight", weight, {D}, at::kFloat, x);
+        expect("branch_weight", branch_weight, {D}, at::kFloat, x);
+        if (weight && !norm_stream) throw Failure(LBSCAN_EINVAL, "weight belongs to the norm of the stream");
+        a.dim = size32("x", D);
+        a.rows = D ? x.numel() / D : 0;
+        a.norm_branch = norm_branch;
+        a.norm_stream = norm_stream;
+        a.eps = (float)eps;
+        a.residual_scale = (float)residual_scale;
+        a.x = x.data_ptr();
+        a.gate = address(gate);
+        a.residual = address<float>(residual);
+        a.branch_weight = address<float>(branch_weight);
+        a.weight = address<float>(weight);
+        return a;
+    }
+};
+
+struct BlockNormResult { Tensor y, sum, rv, rs; };
+BlockNormResult block_norm_run(const BlockNorm& n, bool stats, const Maybe& out, const Stream& stream)
+{
+    lbscan_block_norm_args a = n.args();
+    const Tensor& x = n.x;
+    c10::DeviceGuard guard(x.device());
+    expect("out", out, x.sizes(), x.scalar_type(), x);
+    expect_writable("out", out);
+    expect_apart(out, x, "x");
+    expect_apart(out, n.gate, "the gate");
+    expect_apart(out, n.residual, "the residual");
+    BlockNormResult r;
+    r.y = out ? *out : fresh(stream, x.sizes(), x, x.scalar_type());
+    if (n.residual) r.sum = fresh(stream, x.sizes(), x, at::kFloat);
+    if (stats) {
+        const auto rows = x.sizes().slice(0, x.dim() - 1);
+        for (auto [wanted, t] : {std::pair{n.norm_branch, &r.rv}, std::pair{n.norm_stream, &r.rs}}) {
+            if (!wanted) continue;
+            *t = fresh(stream, rows, x, at::kFloat);
+            if (x.size(-1) == 0) {                       // rows of no columns: no kernel runs
+                c10::OptionalStreamGuard on;
+                if (stream.named) on.reset_stream(*stream.named);
+                t->zero_();
+            }
+        }
+    }
+    a.y = r.y.data_ptr();
+    a.sum = address<float>(r.sum);
+    a.branch_rstd = address<float>(r.rv);
+    a.stream_rstd = address<float>(r.rs);
+    check(lbscan_block_norm_fwd(&a, stream.raw), "lbscan_block_norm_fwd");
+    written(out);
+    return r;
+}
+
+py::object block_norm_fwd(Tensor x, Maybe weight, Maybe gate, Maybe branch_weight, Maybe residual, double residual_scale, bool norm_branch,
+                          bool norm_stream, double eps, bool stats, Maybe out, py::object stream)
+{
+    const BlockNormResult r = block_norm_run({x, weight, gate, branch_weight, residual, residual_scale, norm_branch, norm_stream, eps},
+                                             stats, out, Stream(stream, x));
+    if (!stats) return residual ? py::object(py::make_tuple(r.y, r.sum)) : py::cast(r.y);
+    const py::tuple s = py::make_tuple(maybe(r.rv), maybe(r.rs));
+    return residual ? py::make_tuple(r.y, r.sum, s[0], s[1]) : py::make_tuple(r.y, s[0], s[1]);
+}
+
+struct BlockNormGradients { Tensor dx, dgate, dresidual, dweight, dbranch; };
+// n.residual: the sum that the forward call returned
+BlockNormGradients block_norm_gradients(const BlockNorm& n, const Tensor& dout, const Maybe& dsum, const Maybe& rv, const Maybe& rs,
+                                        bool with_weight, bool with_branch, const Stream& stream)
+{
+    lbscan_block_norm_args a = n.args();
+    const Tensor& x = n.x;
+    c10::DeviceGuard guard(x.device());
+    const auto rows = x.sizes().slice(0, x.dim() - 1);
+    expect("dout", dout, x.sizes(), x.scalar_type(), x);
+    if (dsum && !n.residual) throw Failure(LBSCAN_EINVAL, "dsum belongs to a sum");
+    expect("dsum", dsum, x.sizes(), at::kFloat, x);
+    if (n.norm_branch != (bool)rv || n.norm_stream != (bool)rs)
+        throw Failure(LBSCAN_EINVAL, "branch_rstd and stream_rstd: expected those of the norms that there are");
+    expect("branch_rstd", rv, rows, at::kFloat, x);
+    expect("stream_rstd", rs, rows, at::kFloat, x);
+    a.sum = const_cast<float*>(a.residual);
+    a.branch_rstd = address<float>(rv);
+    a.stream_rstd = address<float>(rs);
+    BlockNormGradients g;
+    g.dx = fresh(stream, x.sizes(), x, x.scalar_type());
+    if (n.gate) g.dgate = fresh(stream, x.sizes(), x, x.scalar_type());
+    if (n.residual) g.dresidual = fresh(stream, x.sizes(), x, at::kFloat);
+    if (with_weight) g.dweight = fresh(stream, {x.size(-1)}, x, at::kFloat);
+    if (with_branch) g.dbranch = fresh(stream, {x.size(-1)}, x, at::kFloat);
+    const size_t need = lbscan_block_norm_workspace_bytes(&a);
+    const Tensor ws = scratch(stream, need, x);
+    a.workspace = address(ws);
+    a.workspace_bytes = need;
+    check(lbscan_block_norm_bwd(&a, dout.data_ptr(), address<float>(dsum), g.dx.data_ptr(), address(g.dgate), address<float>(g.dresidual),
+                                address<float>(g.dweight), address<float>(g.dbranch), stream.raw),
+          "lbscan_block_norm_bwd");
+    return g;
+}
+
+py::dict block_norm_bwd(Tensor x, Maybe weight, Tensor dout, Maybe gate, Maybe branch_weight, Maybe total, Maybe dsum, Maybe rv, Maybe rs,
+                        double residual_scale, bool norm_branch, bool norm_stream, py::object stream)
+{
+    const BlockNormGradients g =
+        block_norm_gradients({x, weight, gate, branch_weight, total, residual_scale, norm_branch, norm_stream, 0.0}, dout, dsum, rv, rs,
+                             (bool)weight, (bool)branch_weight, Stream(stream, x));
+    py::dict r;
+    r["dx"] = g.dx;
+    r["dgate"] = maybe(g.dgate);
+    r["dresidual"] = maybe(g.dresidual);
+    r["dweight"] = maybe(g.dweight);
+    r["dbranch_weight"] = maybe(g.dbranch);
+    return r;
+}
+
+struct BlockNormNode : torch::autograd::Function<BlockNormNode> {
+    static variable_list forward(AutogradContext* ctx, Tensor x, Maybe weight, Maybe gate, Maybe branch_weight, Maybe residual,
+                                 double residual_scale, bool norm_branch, bool norm_stream, double eps)
+    {
+        x = x.contiguous();
+        if (gate) gate = gate->contiguous();
+        if (residual) residual = residual->contiguous();
+        if (!x.is_cuda()) throw Failure(LBSCAN_EINVAL, "x must be a device tensor");
+        const BlockNormResult r = block_norm_run({x, weight, gate, branch_weight, residual, residual_scale, norm_branch, norm_stream, eps},
+                                                 true, {}, Stream(x));
+        ctx->save_for_backward({x, tensor(weight), tensor(gate), tensor(branch_weight), r.sum, r.rv, r.rs});
+        ctx->saved_data["residual_scale"] = residual_scale;
+        ctx->saved_data["norm_branch"] = norm_branch;
+        ctx->saved_data["norm_stream"] = norm_stream;
+        ctx->set_materialize_grads(false);
+        return residual ? variable_list{r.y, r.sum} : variable_list{r.y};
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grads)
+    {
+        return backward_pass([&] { return gradients(ctx, grads); });
+    }
+    static variable_list gradients(AutogradContext* ctx, const variable_list& grads)
+    {
+        refuse_second_derivatives();
+        const auto s = ctx->get_saved_variables();
+        Tensor dout = grads[0], dsum = grads.size() > 1 ? grads[1] : Tensor();
+        variable_list r(9);
+        if (!dout.defined() && !dsum.defined()) return r;
+        dout = dout.defined() ? dout.contiguous() : at::zeros_like(s[0]);
+        if (dsum.defined()) dsum = dsum.contiguous();
+        const BlockNormGradients g = block_norm_gradients(
+            {s[0], maybe(s[1]), maybe(s[2]), maybe(s[3]), maybe(s[4]), ctx->saved_data["residual_scale"].toDouble(),
+             ctx->saved_data["norm_branch"].toBool(), ctx->saved_data["norm_stream"].toBool(), 0.0},
+            dout, maybe(dsum), maybe(s[5]), maybe(s[6]), s[1].defined(), s[3].defined(), Stream(s[0]));
+        r[0] = g.dx; r[1] = g.dweight; r[2] = g.dgate; r[3] = g.dbranch; r[4] = g.dresidual;
+        return r;
+    }
+};
+
+py::object block_norm(Tensor x, Maybe weight, Maybe gate, Maybe branch_weight, Maybe residual, double residual_scale, bool norm_branch,
+                      bool norm_stream, double eps)
+{
+    const auto r = BlockNormNode::apply(x, weight, gate, branch_weight, residual, residual_scale, norm_branch, norm_stream, eps);
+    return r.size() > 1 ? py::object(py::make_tuple(r[0], r[1])) : py::cast(r[0]);
+}
+
+}  // namespace
+
+void define_blocks(py::module_& m)
+{
+    m.def("step", step);
+    m.def("conv1d_prompt", conv1d_prompt);
+    m.def("block_norm_fwd", block_norm_fwd);
+    m.def("block_norm_bwd", block_norm_bwd);
+    m.def("block_norm", block_norm);
+}
+
+}  // namespace lbscan_torch

@@ -1,5 +1,6 @@
-"""Operators of recurrent sequence models around the scan: gated linear recurrence, layer norm, token
-embedding.  Names and defaults only: arguments are checked and the calls made in csrc/lbscan_torch.cpp, and every
+"""Operators of recurrent and state space sequence models around the scan: gated linear recurrence, layer norm, token
+embedding; the scan's and the convolution's forms for serving, the norms around a block.  Names and defaults
+only: arguments are checked and the calls made in csrc/lbscan_torch*.cpp, and every
 value is computed by the HIP kernels behind include/lbscan.h, which defines what each call returns.
 Refused arguments raise binding.LbscanError.
 
@@ -8,7 +9,7 @@ caller sees to it that the inputs (and tensors given to be written) are ready on
 are before they are used on another.  Outputs and scratch are that stream's memory, and outputs are tied to the
 current one.
 
-out, and the state of a single step, are overwritten as in-place operations overwrite: autograd sees it by their versions, and
+out, and the states of steps and prompts, are overwritten as in-place operations overwrite: autograd sees it by their versions, and
 tensors that require gradients are refused while gradients are recorded."""
 from __future__ import annotations
 
@@ -89,3 +90,47 @@ def lbscan_embed_bwd(ids, *, dout, vocab, scale=1.0, stream=None):
     """Gradient of lbscan_embed_fwd with respect to the whole table, (vocab, dim) in dout's type: sums
     over the tokens of each row in fp32 and in the order of the tokens."""
     return (_ext or load()).embed_bwd(ids, dout, vocab, scale, stream)
+
+
+def lbscan_step(x, delta, A, Bm, Cm, state, Dskip=None, z=None, delta_bias=None, *, delta_softplus=True, conv_state=None,
+                conv_weight=None, conv_bias=None, activation=True, slots=None, out=None, stream=None):
+    """One token of every sequence through the selective scan: x, delta, z (B,D), Bm, Cm (B,N), which may be columns of
+    wider tensors, A (D,N), state (B,D,N) fp32, which is updated in place.  With conv_weight (D,K) x goes through the
+    convolution (and SiLU, unless activation is off) first, whose last K-1 inputs are conv_state (B,D,K-1) in x's type, updated in
+    place too.  slots (B) int32: rows of larger states, (S,D,N) and (S,D,K-1), that belong to the rows of x; a row whose slot
+    is none of them, or an earlier row's, is padding: its output is zero and no state is touched for it.  The
+    result is the output (B,D)."""
+    return (_ext or load()).step(x, delta, A, Bm, Cm, state, Dskip, z, delta_bias, delta_softplus, conv_state, conv_weight,
+                                 conv_bias, activation, slots, out, stream)
+
+
+def lbscan_conv1d_step(x, state, weight, bias=None, *, activation=True, slots=None, out=None, stream=None):
+    """One token of every sequence through the convolution: x (B,D), which may be columns of a wider tensor; state and
+    slots as conv_state and slots of lbscan_step."""
+    return (_ext or load()).conv1d_prompt(x, state, weight, bias, activation, None, slots, out, True, stream)
+
+
+def lbscan_conv1d_prompt(x, state, weight, bias=None, *, activation=True, lengths=None, slots=None, out=None, stream=None):
+    """Prompts, or pieces of them, through the convolution: x (B,D,L); the K-1 tokens before them are those of state
+    (zeros before a sequence), which leaves with the last K-1 inputs.  lengths (B) int32: tokens of each row that are there; the
+    output is zero behind them.  state and slots as conv_state and slots of lbscan_step."""
+    return (_ext or load()).conv1d_prompt(x, state, weight, bias, activation, lengths, slots, out, False, stream)
+
+
+def lbscan_block_norm_fwd(x, weight=None, *, gate=None, branch_weight=None, residual=None, residual_scale=1.0,
+                          norm_branch=False, norm_stream=True, eps=1e-5, return_stats=False, out=None, stream=None):
+    """The norms (root mean square) around a block over the last axis of x, its output: x SiLU(gate), normalised with
+    norm_branch, times branch_weight, is added to residual_scale * residual (fp32), and the sum, normalised with norm_stream
+    and times weight, is returned; with a residual (y, sum), the sum in fp32.  branch_weight, weight (dim) fp32.  With
+    return_stats the reciprocal deviations of the branch and of the stream follow (None without the norm)."""
+    return (_ext or load()).block_norm_fwd(x, weight, gate, branch_weight, residual, residual_scale, norm_branch, norm_stream,
+                                           eps, return_stats, out, stream)
+
+
+def lbscan_block_norm_bwd(x, weight=None, *, dout, gate=None, branch_weight=None, total=None, dsum=None, branch_rstd=None,
+                          stream_rstd=None, residual_scale=1.0, norm_branch=False, norm_stream=True, stream=None):
+    """Gradients of lbscan_block_norm_fwd: a dict with dx, dgate, dresidual (fp32), dweight, dbranch_weight, None for what the
+    forward call did not have.  total: the sum that it returned; dsum: the gradient arriving at it; branch_rstd,
+    stream_rstd: its statistics."""
+    return (_ext or load()).block_norm_bwd(x, weight, dout, gate, branch_weight, total, dsum, branch_rstd, stream_rstd,
+                                           residual_scale, norm_branch, norm_stream, stream)
