@@ -315,7 +315,7 @@ int lbscan_embed_bwd(const lbscan_embed_args *fwd_args, const void *dout, void *
                      void *hip_stream);
 size_t lbscan_embed_workspace_bytes(const lbscan_embed_args *args);
 
-/* ---- State space language models: serving, the norms around a block -----------------
+/* ---- State space language models: serving, the norms around a block, the loss --------
  * As above: storage types, ownership, streams and errors, sums in fp32 and in a fixed order. */
 
 /* One token of every sequence through the scan (window 1: a single token has no local backward part) and, with
@@ -413,6 +413,40 @@ int lbscan_block_norm_bwd(const lbscan_block_norm_args *fwd_args, const void *do
                           void *dx, void *dgate, float *dresidual, float *dweight, float *dbranch, void *hip_stream);
 
 size_t lbscan_block_norm_workspace_bytes(const lbscan_block_norm_args *args);
+
+/* Softmax cross entropy of tokens over a vocabulary, the product with the table included and the logits never kept:
+ *     l[t,v] = scale * sum_d x[t,d] weight[v,d]
+ *     lse[t] = log(sum_v exp(l[t,v]))          loss[t] = lse[t] - l[t,targets[t]]
+ * A token whose target is outside [0, vocab) (padding, a prompt) is left out: its loss, lse and dx are zeros, it has no part in
+ * dweight, and its row of x is not looked at.  Logits, maxima and sums are fp32.  The gradients are
+ *     G[t,v] = (dloss[t] + dlse[t]) exp(l[t,v] - lse[t]) - dloss[t] (v == targets[t])
+ *     dx[t,:] = scale * sum_v G[t,v] weight[v,:]      dweight[v,:] = scale * sum_t G[t,v] x[t,:]
+ * with G made again in pieces of the vocabulary, in the storage type (a factor of the products, as x and weight are), and both
+ * sums in fp32. */
+typedef struct lbscan_loss_args {
+    int64_t tokens;               /* <= 2^24; 0: only zeros are written to dweight */
+    int32_t vocab, dim;           /* vocab < 2^30; dim in 1 .. 65536 */
+    int32_t dtype;                /* storage type of x, weight and their gradients */
+    int32_t ids_type;             /* LBSCAN_IDS_* */
+    float scale;                  /* finite */
+    const void *x;                /* (tokens, dim) */
+    const void *weight;           /* (vocab, dim).  Rows of whole 128 bytes from an address that 16 divides are read in
+                                     place, others are copied to the workspace first */
+    const void *targets;          /* (tokens) */
+    float      *loss;             /* (tokens) out of the forward call */
+    float      *lse;              /* (tokens) out of the forward call, read by the backward call */
+    void       *workspace;        /* lbscan_loss_workspace_bytes(args, LBSCAN_WS_FWD / _BWD), address a multiple of 16 */
+    size_t      workspace_bytes;
+} lbscan_loss_args;
+
+int lbscan_loss_fwd(const lbscan_loss_args *args, void *hip_stream);
+
+/* dloss, dlse: the gradients of loss and lse, NULL: zeros.  dx (tokens, dim), dweight (vocab, dim), each NULL: not wanted. */
+int lbscan_loss_bwd(const lbscan_loss_args *fwd_args, const float *dloss, const float *dlse, void *dx, void *dweight,
+                    void *hip_stream);
+
+/* which: LBSCAN_WS_FWD, or LBSCAN_WS_BWD (enough for both gradients).  weight is looked at for its alignment. */
+size_t lbscan_loss_workspace_bytes(const lbscan_loss_args *args, int which);
 
 /* Bytes of device scratch the call named by `which` (LBSCAN_WS_*) needs for
  * these sizes; 0 means workspace may be NULL. */

@@ -107,3 +107,11 @@ def block_norm(x, weight=None, *, gate=None, branch_weight=None, residual=None, 
     """Differentiable norms around a block, with its gate and its residual stream (see lbscan_block_norm_fwd): returns
     y, or (y, sum) with a residual, the sum in fp32."""
     return sequence.load().block_norm(x, weight, gate, branch_weight, residual, residual_scale, norm_branch, norm_stream, eps)
+
+
+def linear_cross_entropy(x, weight, targets, *, scale=1.0):
+    """Differentiable softmax cross entropy of tokens over a vocabulary, without keeping the logits scale * x weight^T: x
+    (..., dim), weight (vocab, dim) in one type, targets (...) int32 or int64.  Returns (loss, lse), fp32 in the shape of targets,
+    zeros (and no gradient) for tokens whose target is no row of the table; the mean over the others is
+    loss.sum() / their number."""
+    return sequence.load().loss(x, weight, targets, scale)

@@ -29,6 +29,7 @@ EXPORTS = (
     "lbscan_embed_fwd", "lbscan_embed_bwd", "lbscan_embed_workspace_bytes",
     "lbscan_step", "lbscan_conv1d_prompt",
     "lbscan_block_norm_fwd", "lbscan_block_norm_bwd", "lbscan_block_norm_workspace_bytes",
+    "lbscan_loss_fwd", "lbscan_loss_bwd", "lbscan_loss_workspace_bytes",
 )
 
 
@@ -122,6 +123,17 @@ class LbscanBlockNormArgs(ctypes.Structure):
     ]
 
 
+class LbscanLossArgs(ctypes.Structure):
+    """Mirror of struct lbscan_loss_args."""
+    _fields_ = [
+        ("tokens", ctypes.c_int64), ("vocab", ctypes.c_int32), ("dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("ids_type", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("x", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("targets", ctypes.c_void_p),
+        ("loss", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
 class LbscanError(RuntimeError):
     def __init__(self, code: int, what: str):
         self.code = code
@@ -165,14 +177,15 @@ def load():
         call.restype = ctypes.c_int
         call.argtypes = [ctypes.POINTER(struct_type), vp]
     for name, struct_type, tensors in (("gated", LbscanGatedArgs, 7), ("norm", LbscanNormArgs, 6),
-                                       ("embed", LbscanEmbedArgs, 2), ("block_norm", LbscanBlockNormArgs, 7)):
+                                       ("embed", LbscanEmbedArgs, 2), ("block_norm", LbscanBlockNormArgs, 7),
+                                       ("loss", LbscanLossArgs, 4)):
         sp = ctypes.POINTER(struct_type)
         fwd, bwd, size = (getattr(lib, f"lbscan_{name}_{what}") for what in ("fwd", "bwd", "workspace_bytes"))
         fwd.restype = bwd.restype = ctypes.c_int
         fwd.argtypes = [sp, vp]
         bwd.argtypes = [sp] + [vp] * (tensors + 1)
         size.restype = ctypes.c_size_t
-        size.argtypes = [sp, ctypes.c_int] if name == "gated" else [sp]
+        size.argtypes = [sp, ctypes.c_int] if name in ("gated", "loss") else [sp]
     lib.lbscan_workspace_bytes.restype = ctypes.c_size_t
     lib.lbscan_workspace_bytes.argtypes = [ap, ctypes.c_int]
     lib.lbscan_default_window.restype = ctypes.c_int

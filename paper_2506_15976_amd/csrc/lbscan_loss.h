@@ -1,0 +1,55 @@
+// Softmax cross entropy over a vocabulary with the product of rows and table included: what its kernels, its plan and the
+// entry points share.  With l_tv = scale x_t . W_v:
+//     lse_t = log sum_v exp l_tv        loss_t = lse_t - l_t,target(t)
+//     G_tv = (g_t + e_t) exp(l_tv - lse_t) - g_t [v = target(t)],   g, e: gradients of loss and lse
+//     dx_t = scale sum_v G_tv W_v       dW_v = scale sum_t G_tv x_t
+// Tokens whose target is no row of the table are left out of all of it: the others (the live ones) are packed together first.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "lbscan_loss_plan.h"
+
+namespace lbscan {
+
+struct LossParams {
+    long tokens;
+    int vocab, dim, dtype, wide_ids;
+    float scale;
+    const void *x, *weight, *targets;
+    float *loss, *lse;                // backward: lse is read
+    const float *dloss, *dlse;        // nullable: zeros
+    void *dx, *dweight;               // nullable
+};
+
+LossPlan loss_plan(const LossParams& p, bool backward);
+hipError_t launch_loss_fwd(const LossParams& p, const LossPlan& plan, void* workspace, hipStream_t stream);
+hipError_t launch_loss_bwd(const LossParams& p, const LossPlan& plan, void* workspace, hipStream_t stream);
+
+// The products' launches, one translation unit for each storage type (lbscan_loss_tile.inc).
+struct LossTiles {
+    const int* live;                  // number of live tokens
+    const void* w;                    // (vocab, ldw), rows of whole steps along dim
+    const void* x;                    // (rows, dimp): the live rows, then zeros to a whole tile
+    void* g;                          // (rows, piece)
+    const int* targets;               // (rows)
+    const float *lse2, *down, *both;  // (rows) lse log2(e), g, g + e; zeros behind the live ones
+    float* own;                       // (rows) l of the target
+    float2* part;                     // (chunks, rows) maximum and sum of a chunk of the vocabulary
+    float* acc;                       // (splits_x, rows, dimp)
+    float* share;                     // (splits_w, piece, dimp)
+    void* dweight;
+    long rows;
+    int vocab, dim, dimp, ldw, piece;
+    int first, count;                 // columns of the vocabulary that this launch has
+    int chunk;                        // tiles of the vocabulary a block (loss and G)
+    int splits;
+    int add;                          // dx: added to what is there
+    float scale;
+};
+enum class LossKind { lse, slope, dx, dweight };
+hipError_t launch_loss_tiles_f32(LossKind kind, const LossTiles& p, int few, hipStream_t stream);
+hipError_t launch_loss_tiles_bf16(LossKind kind, const LossTiles& p, int few, hipStream_t stream);
+
+}  // namespace lbscan

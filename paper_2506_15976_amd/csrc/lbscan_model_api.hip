@@ -1,8 +1,10 @@
-// C entry points of the operators of state space language models (single steps and prompts, norms around a block):
+// C entry points of the operators of state space language models (single steps and prompts, norms around a block, the
+// loss over the vocabulary):
 // argument checks and the launches of a call.  Everything a kernel's indexing assumes is checked here first.
 #include "../../include/lbscan.h"
 #include "lbscan_block_norm.h"
 #include "lbscan_internal.h"
+#include "lbscan_loss.h"
 #include "lbscan_step.h"
 
 #include <math.h>
@@ -56,6 +58,36 @@ lbscan::BlockNormParams block_norm_params(const lbscan_block_norm_args* a)
     p.y = a->y; p.sum = a->sum; p.rv = a->branch_rstd; p.rs = a->stream_rstd;
     p.with_residual = a->residual != nullptr;
     return p;
+}
+
+int check_loss(const lbscan_loss_args* a)
+{
+    if (!a) return LBSCAN_EINVAL;
+    if (a->tokens < 0 || a->vocab < 0 || a->dim < 0) return LBSCAN_EINVAL;
+    if (!known_type(a->dtype)) return LBSCAN_EUNSUPPORTED;
+    if (a->ids_type != LBSCAN_IDS_INT32 && a->ids_type != LBSCAN_IDS_INT64) return LBSCAN_EUNSUPPORTED;
+    if (!isfinite(a->scale)) return LBSCAN_EINVAL;
+    if (a->tokens > (1 << 24) || a->vocab >= (1 << 30) || a->dim < 1 || a->dim > 65536) return LBSCAN_EUNSUPPORTED;
+    return LBSCAN_OK;
+}
+lbscan::LossParams loss_params(const lbscan_loss_args* a)
+{
+    lbscan::LossParams p{};
+    p.tokens = a->tokens; p.vocab = a->vocab; p.dim = a->dim; p.dtype = a->dtype;
+    p.wide_ids = a->ids_type == LBSCAN_IDS_INT64; p.scale = a->scale;
+    p.x = a->x; p.weight = a->weight; p.targets = a->targets;
+    p.loss = a->loss; p.lse = a->lse;
+    return p;
+}
+bool good_loss_inputs(const lbscan_loss_args* a)
+{
+    const size_t e = element_bytes(a->dtype);
+    return good(a->x, e) && good(a->weight, e, a->vocab == 0) && good(a->targets, a->ids_type == LBSCAN_IDS_INT64 ? 8 : 4) && good(a->lse, 4);
+}
+size_t loss_bytes(const lbscan::LossParams& p, const lbscan::LossPlan& plan) { return p.tokens && p.vocab ? plan.total : 0; }
+bool enough_wide(const void* workspace, size_t have, size_t need)
+{
+    return need == 0 || (workspace && have >= need && aligned_to(workspace, 16));
 }
 
 }  // namespace
@@ -167,6 +199,42 @@ size_t lbscan_block_norm_workspace_bytes(const lbscan_block_norm_args* args)
 {
     if (check_block_norm(args) != LBSCAN_OK || args->rows == 0 || args->dim == 0) return 0;
     return lbscan::block_norm_bwd_floats(block_norm_params(args)) * sizeof(float);
+}
+
+int lbscan_loss_fwd(const lbscan_loss_args* args, void* hip_stream)
+{
+    const int rc = check_loss(args);
+    if (rc != LBSCAN_OK) return rc;
+    if (args->tokens == 0) return LBSCAN_OK;
+    if (!good_loss_inputs(args) || !good(args->loss, 4)) return LBSCAN_EINVAL;
+    const lbscan::LossParams p = loss_params(args);
+    const lbscan::LossPlan plan = lbscan::loss_plan(p, false);
+    if (!enough_wide(args->workspace, args->workspace_bytes, loss_bytes(p, plan))) return LBSCAN_EWORKSPACE;
+    return done(lbscan::launch_loss_fwd(p, plan, args->workspace, static_cast<hipStream_t>(hip_stream)), "lbscan_loss_fwd");
+}
+
+int lbscan_loss_bwd(const lbscan_loss_args* args, const float* dloss, const float* dlse, void* dx, void* dweight, void* hip_stream)
+{
+    const int rc = check_loss(args);
+    if (rc != LBSCAN_OK) return rc;
+    const size_t e = element_bytes(args->dtype);
+    if (!good(dweight, e, true) || !good(dx, e, true)) return LBSCAN_EINVAL;
+    if (args->tokens && (!good_loss_inputs(args) || !good(dloss, 4, true) || !good(dlse, 4, true))) return LBSCAN_EINVAL;
+    lbscan::LossParams p = loss_params(args);
+    p.dloss = dloss; p.dlse = dlse; p.dx = dx; p.dweight = dweight;
+    if (!dx && !dweight) return LBSCAN_OK;
+    const lbscan::LossPlan plan = lbscan::loss_plan(p, true);
+    if (!enough_wide(args->workspace, args->workspace_bytes, loss_bytes(p, plan))) return LBSCAN_EWORKSPACE;
+    return done(lbscan::launch_loss_bwd(p, plan, args->workspace, static_cast<hipStream_t>(hip_stream)), "lbscan_loss_bwd");
+}
+
+size_t lbscan_loss_workspace_bytes(const lbscan_loss_args* args, int which)
+{
+    if (check_loss(args) != LBSCAN_OK || (which != LBSCAN_WS_FWD && which != LBSCAN_WS_BWD)) return 0;
+    lbscan::LossParams p = loss_params(args);
+    char wanted;
+    p.dx = p.dweight = &wanted;                        // (never written: both gradients are planned for)
+    return loss_bytes(p, lbscan::loss_plan(p, which == LBSCAN_WS_BWD));
 }
 
 }  // extern "C"

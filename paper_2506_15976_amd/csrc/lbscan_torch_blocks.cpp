@@ -1,5 +1,5 @@
-// The operators of state space language models for torch (single steps and prompts, norms around a block): argument
-// checks, outputs and scratch, autograd nodes.  No arithmetic: every value is computed by the kernels behind include/lbscan.h.
+// The operators of state space language models for torch (single steps and prompts, norms around a block, the loss):
+// argument checks, outputs and scratch, autograd nodes.  No arithmetic: every value is computed by the kernels behind include/lbscan.h.
 #include "lbscan_torch.h"
 
 namespace lbscan_torch {
@@ -322,10 +322,124 @@ py::object block_norm(Tensor x, Maybe weight, Maybe gate, Maybe branch_weight, M
     return r.size() > 1 ? py::object(py::make_tuple(r[0], r[1])) : py::cast(r[0]);
 }
 
+// ---- loss over the vocabulary ----------------------------------------------------------------------------------
+lbscan_loss_args loss_args(const Tensor& x, const Tensor& weight, const Tensor& targets, double scale)
+{
+    lbscan_loss_args a{};
+    expect_axes("weight", weight, 2);
+    if (x.dim() < 1) throw Failure(LBSCAN_EINVAL, "x needs an axis of rows' elements");
+    const auto type = targets.scalar_type();
+    if (type != at::kLong && type != at::kInt)
+        throw Failure(LBSCAN_EUNSUPPORTED, std::string("targets: expected int32 or int64, got ") + c10::toString(type));
+    a.dtype = type_code("x", x.scalar_type());
+    expect("x", x, x.sizes(), x.scalar_type(), x);
+    expect("weight", weight, {weight.size(0), x.size(-1)}, x.scalar_type(), x);
+    expect("targets", targets, x.sizes().slice(0, x.dim() - 1), type, x);
+    a.ids_type = type == at::kLong ? LBSCAN_IDS_INT64 : LBSCAN_IDS_INT32;
+    a.tokens = targets.numel();
+    a.vocab = size32("weight", weight.size(0));
+    a.dim = size32("x", x.size(-1));
+    a.scale = (float)scale;
+    a.x = x.data_ptr(); a.weight = weight.data_ptr(); a.targets = targets.data_ptr();
+    return a;
+}
+
+std::pair<Tensor, Tensor> loss_run(const Tensor& x, const Tensor& weight, const Tensor& targets, double scale, const Stream& stream)
+{
+    lbscan_loss_args a = loss_args(x, weight, targets, scale);
+    c10::DeviceGuard guard(x.device());
+    Tensor loss = fresh(stream, targets.sizes(), x, at::kFloat), lse = fresh(stream, targets.sizes(), x, at::kFloat);
+    a.loss = address<float>(loss);
+    a.lse = address<float>(lse);
+    const size_t need = lbscan_loss_workspace_bytes(&a, LBSCAN_WS_FWD);
+    const Tensor ws = scratch(stream, need, x);
+    a.workspace = address(ws);
+    a.workspace_bytes = need;
+    check(lbscan_loss_fwd(&a, stream.raw), "lbscan_loss_fwd");
+    return {loss, lse};
+}
+py::tuple loss_fwd(Tensor x, Tensor weight, Tensor targets, double scale, py::object stream)
+{
+    auto [loss, lse] = loss_run(x, weight, targets, scale, Stream(stream, x));
+    return py::make_tuple(loss, lse);
+}
+
+std::pair<Tensor, Tensor> loss_gradients(const Tensor& x, const Tensor& weight, const Tensor& targets, const Tensor& lse, const Maybe& dloss,
+                                         const Maybe& dlse, double scale, bool want_dx, bool want_dw, const Stream& stream)
+{
+    lbscan_loss_args a = loss_args(x, weight, targets, scale);
+    c10::DeviceGuard guard(x.device());
+    expect("lse", lse, targets.sizes(), at::kFloat, x);
+    expect("dloss", dloss, targets.sizes(), at::kFloat, x);
+    expect("dlse", dlse, targets.sizes(), at::kFloat, x);
+    a.lse = address<float>(lse);
+    Tensor dx, dweight;
+    if (want_dx) dx = fresh(stream, x.sizes(), x, x.scalar_type());
+    if (want_dw) dweight = fresh(stream, weight.sizes(), x, x.scalar_type());
+    const size_t need = lbscan_loss_workspace_bytes(&a, LBSCAN_WS_BWD);
+    const Tensor ws = scratch(stream, need, x);
+    a.workspace = address(ws);
+    a.workspace_bytes = need;
+    check(lbscan_loss_bwd(&a, address<float>(dloss), address<float>(dlse), address(dx), address(dweight), stream.raw), "lbscan_loss_bwd");
+    return {dx, dweight};
+}
+py::dict loss_bwd(Tensor x, Tensor weight, Tensor targets, Tensor lse, Maybe dloss, Maybe dlse, double scale, py::object stream)
+{
+    auto [dx, dweight] = loss_gradients(x, weight, targets, lse, dloss, dlse, scale, true, true, Stream(stream, x));
+    py::dict r;
+    r["dx"] = dx;
+    r["dweight"] = dweight;
+    return r;
+}
+
+struct LossNode : torch::autograd::Function<LossNode> {
+    static variable_list forward(AutogradContext* ctx, Tensor x, Tensor weight, Tensor targets, double scale, bool want_dx, bool want_dw)
+    {
+        x = x.contiguous();
+        weight = weight.contiguous();
+        targets = targets.contiguous();
+        if (!x.is_cuda()) throw Failure(LBSCAN_EINVAL, "x must be a device tensor");
+        auto [loss, lse] = loss_run(x, weight, targets, scale, Stream(x));
+        ctx->save_for_backward({x, weight, targets, lse});
+        ctx->saved_data["scale"] = scale;
+        ctx->saved_data["dx"] = want_dx;
+        ctx->saved_data["dweight"] = want_dw;
+        ctx->set_materialize_grads(false);
+        return {loss, lse};
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grads)
+    {
+        return backward_pass([&] { return gradients(ctx, grads); });
+    }
+    static variable_list gradients(AutogradContext* ctx, const variable_list& grads)
+    {
+        refuse_second_derivatives();
+        const auto s = ctx->get_saved_variables();
+        variable_list r(6);
+        if (!grads[0].defined() && !grads[1].defined()) return r;
+        Maybe dloss, dlse;
+        if (grads[0].defined()) dloss = grads[0].contiguous();
+        if (grads[1].defined()) dlse = grads[1].contiguous();
+        auto [dx, dweight] = loss_gradients(s[0], s[1], s[2], s[3], dloss, dlse, ctx->saved_data["scale"].toDouble(),
+                                            ctx->saved_data["dx"].toBool(), ctx->saved_data["dweight"].toBool(), Stream(s[0]));
+        r[0] = dx;
+        r[1] = dweight;
+        return r;
+    }
+};
+py::tuple loss(Tensor x, Tensor weight, Tensor targets, double scale)
+{
+    const auto r = LossNode::apply(x, weight, targets, scale, x.requires_grad(), weight.requires_grad());
+    return py::make_tuple(r[0], r[1]);
+}
+
 }  // namespace
 
 void define_blocks(py::module_& m)
 {
+    m.def("loss_fwd", loss_fwd);
+    m.def("loss_bwd", loss_bwd);
+    m.def("loss", loss);
     m.def("step", step);
     m.def("conv1d_prompt", conv1d_prompt);
     m.def("block_norm_fwd", block_norm_fwd);

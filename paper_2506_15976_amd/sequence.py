@@ -1,5 +1,5 @@
 """Operators of recurrent and state space sequence models around the scan: gated linear recurrence, layer norm, token
-embedding; the scan's and the convolution's forms for serving, the norms around a block.  Names and defaults
+embedding; the scan's and the convolution's forms for serving, the norms around a block, the loss over a vocabulary.  Names and defaults
 only: arguments are checked and the calls made in csrc/lbscan_torch*.cpp, and every
 value is computed by the HIP kernels behind include/lbscan.h, which defines what each call returns.
 Refused arguments raise binding.LbscanError.
@@ -134,3 +134,16 @@ def lbscan_block_norm_bwd(x, weight=None, *, dout, gate=None, branch_weight=None
     stream_rstd: its statistics."""
     return (_ext or load()).block_norm_bwd(x, weight, dout, gate, branch_weight, total, dsum, branch_rstd, stream_rstd,
                                            residual_scale, norm_branch, norm_stream, stream)
+
+
+def lbscan_loss_fwd(x, weight, targets, *, scale=1.0, stream=None):
+    """Softmax cross entropy of tokens over a vocabulary: x (..., dim), weight (vocab, dim) in one type, targets (...) int32 or
+    int64.  The logits scale * x weight^T are never kept.  The result is (loss, lse), fp32 in the shape of targets; zeros for
+    tokens whose target is no row of the table, which are left out."""
+    return (_ext or load()).loss_fwd(x, weight, targets, scale, stream)
+
+
+def lbscan_loss_bwd(x, weight, targets, *, lse, dloss=None, dlse=None, scale=1.0, stream=None):
+    """Gradients of lbscan_loss_fwd: a dict with dx and dweight, in x's type; lse as it was returned; dloss, dlse fp32: the
+    gradients of loss and lse (None: zeros)."""
+    return (_ext or load()).loss_bwd(x, weight, targets, lse, dloss, dlse, scale, stream)

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2506_15976_amd import binding, sequence
-from paper_2506_15976_amd.autograd import block_norm
+from paper_2506_15976_amd.autograd import block_norm, linear_cross_entropy
 from paper_2506_15976_amd.binding import EINVAL, EUNSUPPORTED, EWORKSPACE, OK, LbscanError
 
 
@@ -44,7 +44,13 @@ def norm(**k):
     return filled(binding.LbscanBlockNormArgs, given, k)
 
 
+def loss(**k):
+    return filled(binding.LbscanLossArgs, dict(tokens=5, vocab=9, dim=64, ids_type=1, scale=1.0, x=P, weight=P, targets=P, loss=P, lse=P), k)
+
+
 def test_struct_layouts():
+    # int64, 4 int32, a float (padded), 5 pointers, (pointer, size)
+    assert ctypes.sizeof(binding.LbscanLossArgs) == 32 + 5 * 8 + 16
     # 8 int32, 5 int64, 14 pointers
     assert ctypes.sizeof(binding.LbscanStepArgs) == 32 + 5 * 8 + 14 * 8
     # 7 int32 (padded), int64, 7 pointers
@@ -118,6 +124,34 @@ def test_norm_backward_refuses(lib):
     assert size(norm(rows=1000, dim=20000)) == (256 * 2 * 20000 + 1000) * 4
 
 
+@pytest.mark.parametrize("fields,code", [
+    (dict(tokens=-1), EINVAL), (dict(vocab=-1), EINVAL), (dict(dim=-1), EINVAL), (dict(dtype=2), EUNSUPPORTED),
+    (dict(ids_type=2), EUNSUPPORTED), (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL),
+    (dict(tokens=(1 << 24) + 1), EUNSUPPORTED), (dict(vocab=1 << 30), EUNSUPPORTED), (dict(dim=0), EUNSUPPORTED),
+    (dict(dim=65537), EUNSUPPORTED),
+    *[(dict([(name, None)]), EINVAL) for name in ("x", "weight", "targets", "loss", "lse")],
+    *[(dict([(name, P + 2)]), EINVAL) for name in ("x", "weight", "targets", "loss", "lse")], (dict(targets=P + 4), EINVAL),
+    (dict(), EWORKSPACE), (dict(workspace=P, workspace_bytes=64), EWORKSPACE), (dict(workspace=P + 8, workspace_bytes=1 << 40), EWORKSPACE),
+    (dict(tokens=0), OK),
+])
+def test_loss_forward_refuses(lib, fields, code):
+    assert lib.lbscan_loss_fwd(loss(**fields), None) == code
+
+
+def test_loss_backward_refuses(lib):
+    room = dict(workspace=P, workspace_bytes=1 << 40)
+    bwd = lambda args, dloss=P, dlse=P, dx=P, dw=P: lib.lbscan_loss_bwd(args, dloss, dlse, dx, dw, None)  # noqa: E731
+    assert bwd(loss()) == EWORKSPACE and bwd(None) == EINVAL and bwd(loss(dim=0, **room)) == EUNSUPPORTED
+    for bad in (dict(dloss=P + 2), dict(dlse=P + 1), dict(dx=P + 2), dict(dw=P + 1)):
+        assert bwd(loss(**room), **bad) == EINVAL, bad
+    assert bwd(loss(lse=None, **room)) == EINVAL and bwd(loss(), dx=None, dw=None) == OK
+    size = lib.lbscan_loss_workspace_bytes
+    assert size(loss(tokens=0), 0) == size(loss(vocab=0), 1) == size(loss(), 7) == size(None, 0) == size(loss(dim=0), 0) == 0
+    # a table whose rows are no whole steps, or that is not aligned, has a copy
+    big = dict(tokens=100, vocab=100000)
+    assert size(loss(dim=64, **big), 0) + 100000 * 64 * 4 == size(loss(dim=64, weight=P + 4, **big), 0) == size(loss(dim=63, **big), 0)
+
+
 def test_tensors_are_refused():
     """(meta and CPU tensors: no call gets as far as the GPU)"""
     cpu = lambda *s, **k: torch.zeros(*s, **k)  # noqa: E731
@@ -132,6 +166,10 @@ def test_tensors_are_refused():
         lambda: sequence.lbscan_block_norm_fwd(cpu(3, 5)),
         lambda: sequence.lbscan_block_norm_fwd(cpu(3, 5).double()),
         lambda: block_norm(cpu(3, 5)),
+        lambda: sequence.lbscan_loss_fwd(cpu(3, 5), cpu(7, 5), cpu(3, dtype=torch.int64)),
+        lambda: sequence.lbscan_loss_fwd(cpu(3, 5), cpu(7, 5), cpu(3)),
+        lambda: sequence.lbscan_loss_fwd(cpu(3, 5).half(), cpu(7, 5).half(), cpu(3, dtype=torch.int64)),
+        lambda: linear_cross_entropy(cpu(3, 5), cpu(7, 5), cpu(3, dtype=torch.int64)),
         lambda: sequence.lbscan_block_norm_bwd(cpu(3, 5), dout=cpu(3, 5)),
     ):
         with pytest.raises(LbscanError):
@@ -181,6 +219,14 @@ class TestOnTheDevice:
                      lambda: sequence.lbscan_block_norm_fwd(y, out=y), lambda: sequence.lbscan_block_norm_fwd(y, gate=t(3, 6)),
                      lambda: sequence.lbscan_block_norm_bwd(y, dout=y), lambda: sequence.lbscan_block_norm_bwd(y, dout=y, stream_rstd=t(4)),
                      lambda: sequence.lbscan_block_norm_bwd(y, dout=y, stream_rstd=t(3), dsum=y),
-                     lambda: sequence.lbscan_block_norm_fwd(t())):
+                     lambda: sequence.lbscan_block_norm_fwd(t()),
+                     lambda: sequence.lbscan_loss_fwd(y, t(7, 4), t(3, dtype=torch.int64)),
+                     lambda: sequence.lbscan_loss_fwd(y, t(7, 5, dtype=torch.bfloat16), t(3, dtype=torch.int64)),
+                     lambda: sequence.lbscan_loss_fwd(y, t(7, 5), t(4, dtype=torch.int64)),
+                     lambda: sequence.lbscan_loss_fwd(y, t(7, 5), t(3, dtype=torch.int16)),
+                     lambda: sequence.lbscan_loss_fwd(y, t(7, 10)[:, :5], t(3, dtype=torch.int64)),
+                     lambda: sequence.lbscan_loss_fwd(t(3, 0), t(7, 0), t(3, dtype=torch.int64)),
+                     lambda: sequence.lbscan_loss_bwd(y, t(7, 5), t(3, dtype=torch.int64), lse=t(4)),
+                     lambda: sequence.lbscan_loss_bwd(y, t(7, 5), t(3, dtype=torch.int64), lse=t(3), dloss=t(3, dtype=torch.bfloat16))):
             with pytest.raises(LbscanError):
                 call()
