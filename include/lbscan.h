@@ -430,7 +430,7 @@ typedef struct lbscan_loss_args {
     int32_t ids_type;             /* LBSCAN_IDS_* */
     float scale;                  /* finite */
     const void *x;                /* (tokens, dim) */
-    const void *weight;           /* (vocab, dim).  Rows of whole 128 bytes from an address that 16 divides are read in
+    const void *weight;           /* (vocab, dim).  Rows of whole 64 bytes from an address that 16 divides are read in
                                      place, others are copied to the workspace first */
     const void *targets;          /* (tokens) */
     float      *loss;             /* (tokens) out of the forward call */

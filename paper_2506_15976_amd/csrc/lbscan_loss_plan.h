@@ -10,7 +10,7 @@ constexpr int kLossFewTokens = 64, kLossFewVocab = 128;
 constexpr int kLossUnits = 256;               // blocks under way at once
 
 struct LossPlan {
-    int dimp;                // dim in whole steps of the products (128 bytes)
+    int dimp;                // dim in whole steps of the products (64 bytes)
     long rows;               // tokens in whole tiles
     int few;                 // tiles of 64 tokens
     int copy_weight;         // the table's rows are no whole steps, or not aligned
@@ -40,7 +40,7 @@ inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool 
 {
     LossPlan p{};
     if (tokens == 0 || vocab == 0 || dim == 0) return p;        // (no kernel runs)
-    const int step = 128 / element;
+    const int step = 64 / element;
     p.dimp = (int)(loss_ceil(dim, step) * step);
     p.few = tokens <= kLossFewTokens;
     p.rows = loss_ceil(tokens, p.few ? kLossFewTokens : kLossTile) * (p.few ? kLossFewTokens : kLossTile);
