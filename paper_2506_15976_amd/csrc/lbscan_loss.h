@@ -29,22 +29,21 @@ hipError_t launch_loss_bwd(const LossParams& p, const LossPlan& plan, void* work
 
 // The products' launches, one translation unit for each storage type (lbscan_loss_tile.inc).
 struct LossTiles {
-    const int* live;                  // number of live tokens
+    const LossChoice* choice;
     const void* w;                    // (vocab, ldw), rows of whole steps along dim
     const void* x;                    // (rows, dimp): the live rows, then zeros to a whole tile
     void* g;                          // (rows, piece)
     const int* targets;               // (rows)
     const float *lse2, *down, *both;  // (rows) lse log2(e), g, g + e; zeros behind the live ones
     float* own;                       // (rows) l of the target
-    float2* part;                     // (chunks, rows) maximum and sum of a chunk of the vocabulary
-    float* acc;                       // (splits_x, rows, dimp)
-    float* share;                     // (splits_w, piece, dimp)
+    float2* part;                     // (chunks, live rows) maximum and sum of a chunk of the vocabulary
+    float* acc;                       // (splits, live rows, dimp)
+    float* share;                     // (splits, count in whole tiles, dimp)
     void* dweight;
     long rows;
     int vocab, dim, dimp, ldw, piece;
     int first, count;                 // columns of the vocabulary that this launch has
-    int chunk;                        // tiles of the vocabulary a block (loss and G)
-    int splits;
+    int last;                         // of the pieces
     int add;                          // dx: added to what is there
     float scale;
 };

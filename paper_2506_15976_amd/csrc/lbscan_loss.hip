@@ -46,8 +46,66 @@ __global__ __launch_bounds__(256) void loss_count_kernel(const Sources s, int* _
     if (threadIdx.x == 0) counts[blockIdx.x] = n;
 }
 
+// How the products are cut.
+struct Cuts {
+    int vocab, dimp, piece, few, element;
+    long part_room, acc_rows, share_rows;
+};
+// The lane's candidate of smallest time, found by a wave.
+__device__ __forceinline__ int best_of(float time, int candidate)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const float other = __shfl_xor(time, m, 64);
+        const int theirs = __shfl_xor(candidate, m, 64);
+        if (other < time || (other == time && theirs < candidate)) { time = other; candidate = theirs; }
+    }
+    return candidate;
+}
+__device__ int best_chunk(int ntiles, int vtiles, int steps, int units, int most_chunks)
+{
+    const int rounds = (threadIdx.x & 63) + 1;
+    int chunk = loss_chunk_of(ntiles, vtiles, rounds, units);
+    if (loss_ceil32(vtiles, chunk) > most_chunks) chunk = loss_ceil32(vtiles, most_chunks);
+    return best_of(loss_chunk_time(ntiles, vtiles, chunk, steps, units), chunk);
+}
+__device__ int best_splits(long tiles, int steps, int units, int element, long most)
+{
+    const int splits = (threadIdx.x & 63) + 1;
+    const bool fits = splits <= kLossMostSplits && loss_split_fits(steps, splits, most);
+    return best_of(fits ? loss_split_time(tiles, steps, splits, units, element) : INFINITY, splits);
+}
+__device__ void choose(LossChoice* out, const Cuts& c, int live)
+{
+    const int ntile = loss_tokens(c.few, c.element), wtile = loss_tokens(0, c.element), vtile = c.few ? kLossFewVocab : kLossTile;
+    const int units = loss_units(c.few), step = 64 / c.element, ntiles = loss_ceil32(live, ntile);
+    LossChoice r{};
+    r.live = live;
+    r.rows = ntiles * ntile;
+    r.chunk_lse = r.chunk_slope[0] = r.chunk_slope[1] = r.splits_x = r.splits_w[0] = r.splits_w[1] = 1;
+    if (live) {
+        const int steps = c.dimp / step, last = c.vocab - (c.vocab - 1) / c.piece * c.piece;
+        if (c.part_room) r.chunk_lse = best_chunk(ntiles, loss_ceil32(c.vocab, vtile), steps, units, (int)(c.part_room / r.rows));
+        else {
+            const long mx = (long)loss_ceil32(c.dimp, vtile) * ntiles, mw = loss_ceil32(c.dimp, kLossTile);
+            const int tokens = loss_ceil32(live, step);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int count = k ? last : c.piece, tiles = loss_ceil32(count, wtile);
+                r.chunk_slope[k] = best_chunk(ntiles, loss_ceil32(count, vtile), steps, units, 1 << 30);
+                r.splits_w[k] = c.share_rows ? best_splits(mw * tiles, tokens, 256, c.element, c.share_rows / ((long)tiles * wtile)) : 1;
+            }
+            // (one number of parts for all pieces: their sums are added to)
+            r.splits_x = best_splits(mx, loss_ceil32(c.piece < c.vocab ? c.piece : c.vocab, step), units, c.element, c.acc_rows / r.rows);
+        }
+    }
+    if ((threadIdx.x & 63) == 0) *out = r;
+}
+
 struct Numbering {
-    int *rank, *order, *targets, *live;
+    int *rank, *order, *targets;
+    LossChoice* choice;
+    Cuts cuts;
     float *lse2, *down, *both;                  // backward
     const float *lse, *dloss, *dlse;
 };
@@ -92,7 +150,8 @@ __global__ __launch_bounds__(256) void loss_rank_kernel(const Sources s, const i
         }
         ++r;
     }
-    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 255) *o.live = r;
+    // (the last thread of the last block has counted them all)
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x >= 192) choose(o.choice, o.cuts, __builtin_amdgcn_readlane(r, 63));
 }
 
 // A wave a row: `dim` elements and zeros up to `dimp`.
@@ -113,10 +172,10 @@ __device__ __forceinline__ void copy_row(T* __restrict__ to, const T* __restrict
 // The live rows one behind the other, then rows of zeros (of no target) to a whole tile.
 template <typename T>
 __global__ __launch_bounds__(256) void loss_gather_kernel(const T* __restrict__ x, T* __restrict__ out, const int* __restrict__ order,
-                                                          int* __restrict__ targets, const int* __restrict__ live_tokens, long rows, int dim,
+                                                          int* __restrict__ targets, const LossChoice* __restrict__ choice, long rows, int dim,
                                                           int dimp, int tile)
 {
-    const int live = *live_tokens;
+    const int live = choice->live;
     const long end = min(rows, ((long)live + tile - 1) / tile * tile);
     for (long r = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < end; r += (long)gridDim.x * 4) {
         const bool there = r < live;
@@ -140,8 +199,9 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2)
 // lse and loss of 16 tokens a block, 16 threads to each.
 __global__ __launch_bounds__(256) void loss_join_kernel(const float2* __restrict__ part, const float* __restrict__ own,
                                                         const int* __restrict__ rank, float* __restrict__ loss, float* __restrict__ lse,
-                                                        long tokens, long rows, int chunks)
+                                                        long tokens, int vtiles, const LossChoice* __restrict__ choice)
 {
+    const long rows = choice->rows, chunks = loss_ceil(vtiles, choice->chunk_lse);
     __shared__ float2 folds[16][17];
     const int at = threadIdx.x & 15, piece = threadIdx.x >> 4;
     for (long first = (long)blockIdx.x * 16; first < tokens; first += (long)gridDim.x * 16) {
@@ -167,44 +227,53 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const float2* __restrict
     }
 }
 
-// dx: the sums' pieces added in their order, in their tokens' places; zeros for the others.  A wave a token.
+// dx: the sums' parts added in their order, in their tokens' places; zeros for the others.  A wave has 256 columns of a token.
 template <typename T>
 __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ acc, const int* __restrict__ rank, T* __restrict__ dx,
-                                                      long tokens, long rows, int dim, int dimp, int splits, float scale)
+                                                      long tokens, int dim, int dimp, const LossChoice* __restrict__ choice, float scale)
 {
-    for (long t = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); t < tokens; t += (long)gridDim.x * 4) {
-        const int r = rank[t];
-        for (int c = (threadIdx.x & 63) * 4; c < dim; c += 256) {
-            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (r >= 0)
-                for (int k = 0; k < splits; ++k) {
-                    const Pack<float, 4> q = *reinterpret_cast<const Pack<float, 4>*>(acc + ((long)k * rows + r) * dimp + c);
+    const long rows = choice->rows;
+    const int splits = choice->splits_x, strips = (dim + 255) / 256;
+    const long all = tokens * strips;
+    for (long w = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); w < all; w += (long)gridDim.x * 4) {
+        const long t = w / strips;
+        const int r = rank[t], c = (int)(w - t * strips) * 256 + (threadIdx.x & 63) * 4;
+        if (c >= dim) continue;
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (r >= 0) {
+#pragma unroll 8
+            for (int k = 0; k < splits; ++k) {
+                const Pack<float, 4> q = *reinterpret_cast<const Pack<float, 4>*>(acc + ((long)k * rows + r) * dimp + c);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] += q.v[i];
-                }
-            Pack<T, 4> o;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o.v[i] = from_f32<T>(v[i] * scale);
-            T* to = dx + t * dim + c;
-            if (c + 4 <= dim) *reinterpret_cast<Pack<T, 4>*>(to) = o;
-            else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (c + i < dim) to[i] = o.v[i];
+                for (int i = 0; i < 4; ++i) v[i] += q.v[i];
             }
+        }
+        Pack<T, 4> o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.v[i] = from_f32<T>(v[i] * scale);
+        T* to = dx + t * dim + c;
+        if (c + 4 <= dim) *reinterpret_cast<Pack<T, 4>*>(to) = o;
+        else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c + i < dim) to[i] = o.v[i];
         }
     }
 }
 // dweight of a piece of the vocabulary, likewise.
 template <typename T>
-__global__ __launch_bounds__(256) void loss_dweight_kernel(const float* __restrict__ share, T* __restrict__ dweight, int count, long piece,
-                                                           int dim, int dimp, int splits, float scale)
+__global__ __launch_bounds__(256) void loss_dweight_kernel(const float* __restrict__ share, T* __restrict__ dweight, int count, int dim, int dimp,
+                                                           const LossChoice* __restrict__ choice, int last, float scale)
 {
+    constexpr int tile = loss_tokens(0, sizeof(T));
+    const long columns = loss_ceil(count, tile) * tile;
+    const int splits = choice->splits_w[last];
+    if (splits == 1) return;                                    // (written by the products)
     for (long v = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); v < count; v += (long)gridDim.x * 4)
         for (int c = (threadIdx.x & 63) * 4; c < dim; c += 256) {
             float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             for (int k = 0; k < splits; ++k) {
-                const Pack<float, 4> q = *reinterpret_cast<const Pack<float, 4>*>(share + (k * piece + v) * dimp + c);
+                const Pack<float, 4> q = *reinterpret_cast<const Pack<float, 4>*>(share + (k * columns + v) * dimp + c);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[i] += q.v[i];
             }
@@ -245,14 +314,15 @@ hipError_t pack(const LossParams& p, const LossPlan& plan, const Scratch& s, boo
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    Numbering o{s.at<int>(plan.rank), s.at<int>(plan.order), s.at<int>(plan.targets), s.at<int>(plan.live), nullptr, nullptr, nullptr,
-                p.lse, p.dloss, p.dlse};
+    Numbering o{s.at<int>(plan.rank), s.at<int>(plan.order), s.at<int>(plan.targets), s.at<LossChoice>(plan.choice),
+                Cuts{p.vocab, plan.dimp, plan.piece, plan.few, (int)sizeof(T), plan.part_room, plan.acc_rows, plan.share_rows},
+                nullptr, nullptr, nullptr, p.lse, p.dloss, p.dlse};
     if (backward) { o.lse2 = s.at<float>(plan.lse2); o.down = s.at<float>(plan.down); o.both = s.at<float>(plan.both); }
     loss_rank_kernel<<<(unsigned)groups, 256, 0, stream>>>(src, counts, o);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    loss_gather_kernel<T><<<some(plan.rows / 4), 256, 0, stream>>>(static_cast<const T*>(p.x), s.at<T>(plan.x), o.order, o.targets, o.live,
-                                                                 plan.rows, p.dim, plan.dimp, plan.few ? kLossFewTokens : kLossTile);
+    loss_gather_kernel<T><<<some(plan.rows / 4), 256, 0, stream>>>(static_cast<const T*>(p.x), s.at<T>(plan.x), o.order, o.targets, o.choice,
+                                                                 plan.rows, p.dim, plan.dimp, loss_tokens(plan.few, sizeof(T)));
     e = hipGetLastError();
     if (e != hipSuccess || !plan.copy_weight) return e;
     loss_rows_kernel<T><<<some((p.vocab + 3L) / 4), 256, 0, stream>>>(static_cast<const T*>(p.weight), s.at<T>(plan.w), p.vocab, p.dim, plan.dimp);
@@ -262,15 +332,14 @@ hipError_t pack(const LossParams& p, const LossPlan& plan, const Scratch& s, boo
 LossTiles tiles_of(const LossParams& p, const LossPlan& plan, const Scratch& s)
 {
     LossTiles t{};
-    t.live = s.at<int>(plan.live);
+    t.choice = s.at<LossChoice>(plan.choice);
     t.w = plan.copy_weight ? s.at<void>(plan.w) : p.weight;
     t.x = s.at<void>(plan.x);
     t.targets = s.at<int>(plan.targets);
     t.rows = plan.rows;
     t.vocab = p.vocab; t.dim = p.dim; t.dimp = plan.dimp; t.ldw = plan.dimp; t.piece = plan.piece;
     t.first = 0; t.count = p.vocab;
-    t.chunk = plan.chunk;
-    t.splits = 1;
+    t.last = 1;
     t.scale = p.scale;
     return t;
 }
@@ -285,8 +354,8 @@ hipError_t forward(const LossParams& p, const LossPlan& plan, const Scratch& s, 
     t.part = s.at<float2>(plan.part);
     e = (sizeof(T) == 4 ? launch_loss_tiles_f32 : launch_loss_tiles_bf16)(LossKind::lse, t, plan.few, stream);
     if (e != hipSuccess) return e;
-    loss_join_kernel<<<some((p.tokens + 15) / 16), 256, 0, stream>>>(t.part, t.own, s.at<int>(plan.rank), p.loss, p.lse, p.tokens, plan.rows,
-                                                                   plan.chunks);
+    loss_join_kernel<<<some((p.tokens + 15) / 16), 256, 0, stream>>>(t.part, t.own, s.at<int>(plan.rank), p.loss, p.lse, p.tokens,
+                                                                   (int)loss_ceil(p.vocab, plan.few ? kLossFewVocab : kLossTile), t.choice);
     return hipGetLastError();
 }
 
@@ -303,25 +372,24 @@ hipError_t backward(const LossParams& p, const LossPlan& plan, const Scratch& s,
     t.dweight = p.dweight;
     for (t.first = 0; t.first < p.vocab && e == hipSuccess; t.first += plan.piece) {
         t.count = p.vocab - t.first < plan.piece ? p.vocab - t.first : plan.piece;
+        t.last = t.first + plan.piece >= p.vocab;
         e = launch(LossKind::slope, t, plan.few, stream);
         if (e == hipSuccess && p.dx) {
-            t.splits = plan.splits_x;
             t.add = t.first > 0;
             e = launch(LossKind::dx, t, plan.few, stream);
         }
         if (e == hipSuccess && p.dweight) {
-            t.splits = plan.splits_w;
             e = launch(LossKind::dweight, t, plan.few, stream);
-            if (e == hipSuccess && plan.splits_w > 1) {
+            if (e == hipSuccess && plan.share_rows) {
                 loss_dweight_kernel<T><<<some((t.count + 3L) / 4), 256, 0, stream>>>(t.share, static_cast<T*>(p.dweight) + (long)t.first * p.dim, t.count,
-                                                                                   plan.piece, p.dim, plan.dimp, plan.splits_w, p.scale);
+                                                                                   p.dim, plan.dimp, t.choice, t.last, p.scale);
                 e = hipGetLastError();
             }
         }
     }
     if (e != hipSuccess || !p.dx) return e;
-    loss_dx_kernel<T><<<some((p.tokens + 3) / 4), 256, 0, stream>>>(t.acc, s.at<int>(plan.rank), static_cast<T*>(p.dx), p.tokens, plan.rows, p.dim,
-                                                                  plan.dimp, plan.splits_x, p.scale);
+    loss_dx_kernel<T><<<some((p.tokens * ((p.dim + 255) / 256) + 3) / 4), 256, 0, stream>>>(t.acc, s.at<int>(plan.rank), static_cast<T*>(p.dx), p.tokens, p.dim, plan.dimp,
+                                                                  t.choice, p.scale);
     return hipGetLastError();
 }
 

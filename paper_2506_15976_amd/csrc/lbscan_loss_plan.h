@@ -1,13 +1,61 @@
-// Sizes, pieces and scratch of a call of the loss.  No device code: the rules hold on the host alone.
+// Sizes, pieces and scratch of a call of the loss, and how its products are cut into the units that blocks take.  How many tokens
+// are live is known on the device alone: the cuts are chosen there, by the same functions, within the room planned here.
 #pragma once
+#include <math.h>
 #include <stddef.h>
 #include <stdint.h>
 
+#ifdef __HIPCC__
+#define LBSCAN_BOTH __host__ __device__
+#else
+#define LBSCAN_BOTH
+#endif
+
 namespace lbscan {
 
-constexpr int kLossTile = 256;                // rows and columns of a block's product
+constexpr int kLossTile = 256;                // rows of the table, or columns of x, of a block's product
 constexpr int kLossFewTokens = 64, kLossFewVocab = 128;
-constexpr int kLossUnits = 256;               // blocks under way at once
+// Tokens (of dweight: rows of the table) of a block's product.  fp32: half as many and two blocks a compute unit, of which one
+// alone keeps the matrix cores as busy: where the last round is not full a compute unit has one.  MI355X, us, logits of
+// 1261 x 32003 x 385: 332 with one block of 256 x 256, 278 with two of 256 x 128; bf16 16384 x 50000 x 768: 1406, 1561.
+LBSCAN_BOTH constexpr int loss_tokens(int few, int element) { return few ? kLossFewTokens : element == 4 ? 128 : 256; }
+constexpr int kLossMostSplits = 32;
+
+// What the device chooses once the live tokens are counted (the start of the scratch).
+struct LossChoice {
+    int live, rows;                           // live tokens; in whole tiles
+    int chunk_lse, chunk_slope[2];            // tiles of the vocabulary a unit: all of it; a piece, the last piece
+    int splits_x, splits_w[2];                // parts of the sums; of dweight for a piece, the last piece
+};
+
+LBSCAN_BOTH inline long loss_ceil(long a, long b) { return (a + b - 1) / b; }
+LBSCAN_BOTH inline int loss_ceil32(int a, int b) { return (a + b - 1) / b; }
+// Compute units, whose rounds of units of the products are counted; of few tokens three blocks run on one at once.
+LBSCAN_BOTH constexpr int loss_units(int few) { return few ? 768 : 256; }
+
+// Time of the logits' products in steps, in units of `chunk` of `vtiles` tiles of the vocabulary for each of `ntiles` tiles of
+// tokens: whole rounds of the machine.  A tile's exponentials take about as long as 6 steps, a unit's first loads 3.
+LBSCAN_BOTH inline float loss_chunk_time(int ntiles, int vtiles, int chunk, int steps, int units)
+{
+    return ceilf((float)ntiles * (float)loss_ceil32(vtiles, chunk) / (float)units) * ((float)chunk * (float)(steps + 6) + 3.0f);
+}
+// The chunk that fills about `rounds` rounds.
+LBSCAN_BOTH inline int loss_chunk_of(int ntiles, int vtiles, int rounds, int units)
+{
+    const int chunks = units * rounds / ntiles;
+    return loss_ceil32(vtiles, chunks < 1 ? 1 : chunks > vtiles ? vtiles : chunks);
+}
+// Time of a sum over `steps` steps for `tiles` tiles, cut into `splits` parts, which are written and read once more (4 bytes a
+// value at about 4.5 TB/s: 0.12 us a tile of 256 x 256, of 1.0 us a step in bf16, 0.06 us one of 256 x 128, of 1.8 us in fp32).
+LBSCAN_BOTH inline float loss_split_time(long tiles, int steps, int splits, int units, int element)
+{
+    const float all = (float)tiles * (float)splits;
+    float rounds = ceilf(all / (float)units);
+    // (fp32: a block alone on its compute unit takes about a quarter longer than half the time of two)
+    if (element == 4 && ceilf(rounds / 2.0f) * 2.0f != rounds) rounds += 0.25f;
+    return rounds * (float)(loss_ceil32(steps, splits) + 4) + (splits > 1 ? (element == 2 ? 0.12f : 0.035f) * all : 0.0f);
+}
+LBSCAN_BOTH inline bool loss_split_fits(int steps, int splits, long most) { return splits == 1 || (splits <= most && splits * 8 <= steps); }
 
 struct LossPlan {
     int dimp;                // dim in whole steps of the products (64 bytes)
@@ -15,24 +63,20 @@ struct LossPlan {
     int few;                 // tiles of 64 tokens
     int copy_weight;         // the table's rows are no whole steps, or not aligned
     int piece, pieces;       // columns of the vocabulary that G has room for
-    int chunk, chunks;       // tiles of the vocabulary a block of the forward pass takes
-    int splits_x, splits_w;
+    long part_room;          // values of the forward pass's parts (rows x chunks)
+    long acc_rows;           // rows of dx's sums (rows x splits)
+    long share_rows;         // rows of dweight's, where it is cut (columns of a piece x splits)
     // bytes from the start of the scratch
-    size_t live, counts, rank, order, targets, lse2, down, both, own, part, x, w, g, acc, share, total;
+    size_t choice, counts, rank, order, targets, lse2, down, both, own, part, x, w, g, acc, share, total;
 };
 
-inline long loss_ceil(long a, long b) { return (a + b - 1) / b; }
-
-// Cuts the sum of a product of `tiles` blocks and `steps` steps so that the blocks are whole rounds of the machine, as
-// far as the pieces' own cost (their sums are written and read once more, about `cost` steps each) allows.
-inline int loss_splits(long tiles, long steps, long cost)
+inline int loss_best_splits(long tiles, int steps, int units, int element)
 {
     int best = 1;
-    long least = -1;
-    for (int s = 1; s <= 16 && (s == 1 || s * 8 <= steps); ++s) {
-        const long time = loss_ceil(tiles * s, kLossUnits) * (loss_ceil(steps, s) + cost);
-        if (least < 0 || time < least) { least = time; best = s; }
-    }
+    for (int s = 2; s <= kLossMostSplits; ++s)
+        if (loss_split_fits(steps, s, kLossMostSplits) &&
+            loss_split_time(tiles, steps, s, units, element) < loss_split_time(tiles, steps, best, units, element))
+            best = s;
     return best;
 }
 
@@ -43,24 +87,23 @@ inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool 
     const int step = 64 / element;
     p.dimp = (int)(loss_ceil(dim, step) * step);
     p.few = tokens <= kLossFewTokens;
-    p.rows = loss_ceil(tokens, p.few ? kLossFewTokens : kLossTile) * (p.few ? kLossFewTokens : kLossTile);
+    const int ntile = loss_tokens(p.few, element), wtile = loss_tokens(0, element), units = loss_units(p.few);
+    p.rows = loss_ceil(tokens, ntile) * ntile;
     p.copy_weight = dim != p.dimp || !aligned;
-    const long width = loss_ceil(vocab, kLossTile) * kLossTile;
-    // G: at most a gigabyte of the vocabulary at a time, in pieces of one size
-    const long most = ((long)1 << 30) / (p.rows * element) / kLossTile * kLossTile;
-    p.pieces = (int)loss_ceil(width, most < kLossTile ? kLossTile : most);
-    p.piece = (int)(loss_ceil(width / kLossTile, p.pieces) * kLossTile);
-    p.pieces = (int)loss_ceil(width, p.piece);
-    // blocks of several tiles of the vocabulary, where there are many
-    const int vtile = p.few ? kLossFewVocab : kLossTile;
-    const long vtiles = loss_ceil(vocab, vtile), ntiles = p.rows / (p.few ? kLossFewTokens : kLossTile);
-    const long per = vtiles * ntiles / (8 * kLossUnits);
-    p.chunk = (int)(per < 1 ? 1 : per > 8 ? 8 : per);
-    p.chunks = (int)loss_ceil(vtiles, p.chunk);
-    p.splits_x = p.splits_w = 1;
+    const long mtiles = loss_ceil(p.dimp, kLossTile), vtiles = loss_ceil(vocab, kLossTile);
+    // G: at most a gigabyte of the vocabulary at a time, in pieces that are just a whole number of rounds of dweight's tiles
+    long most = ((long)1 << 30) / (p.rows * element) / kLossTile;
+    if (most < 1) most = 1;
+    long tiles = vtiles;
+    if (most < vtiles) {
+        tiles = 256 * (most * mtiles / 256) / mtiles;
+        if (tiles < 1) tiles = most;
+    }
+    p.piece = (int)(tiles * kLossTile);
+    p.pieces = (int)loss_ceil(vtiles, tiles);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
-    p.live = take(4);
+    p.choice = take(sizeof(LossChoice));
     p.counts = take(4 * (size_t)loss_ceil(tokens, 1024));
     p.rank = take(4 * (size_t)tokens);
     p.order = take(4 * (size_t)p.rows);
@@ -68,21 +111,30 @@ inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool 
     p.x = take((size_t)p.rows * p.dimp * element);
     if (p.copy_weight) p.w = take((size_t)vocab * p.dimp * element);
     if (!backward) {
+        // chunks for up to 64 rounds of units
+        const long all = p.rows * loss_ceil(vocab, p.few ? kLossFewVocab : kLossTile), room = 64L * units * ntile;
+        p.part_room = all < room ? all : room < p.rows ? p.rows : room;
         p.own = take(4 * (size_t)p.rows);
-        p.part = take(8 * (size_t)p.rows * p.chunks);
+        p.part = take(8 * (size_t)p.part_room);
     } else {
-        const long mtiles = loss_ceil(p.dimp, kLossTile);
         p.lse2 = take(4 * (size_t)p.rows);
         p.down = take(4 * (size_t)p.rows);
         p.both = take(4 * (size_t)p.rows);
         p.g = take((size_t)p.rows * p.piece * element);
         if (want_dx) {
-            p.splits_x = loss_splits(mtiles * ntiles, p.piece / step, 8);
-            p.acc = take(4 * (size_t)p.splits_x * p.rows * p.dimp);
+            // as many parts as all tokens need, and more for fewer live ones
+            const long few_rows = p.few ? 1024 : 8192;
+            p.acc_rows = p.rows * loss_best_splits(loss_ceil(p.dimp, p.few ? kLossFewVocab : kLossTile) * (p.rows / ntile), (int)loss_ceil(p.piece, step), units, element);
+            if (p.acc_rows < few_rows) p.acc_rows = few_rows;
+            p.acc = take(4 * (size_t)p.acc_rows * p.dimp);
         }
         if (want_dw) {
-            p.splits_w = loss_splits(mtiles * (p.piece / kLossTile), loss_ceil(p.rows, step), 8);
-            if (p.splits_w > 1) p.share = take(4 * (size_t)p.splits_w * p.piece * p.dimp);
+            const int steps = (int)loss_ceil(p.rows, step);
+            const long last = loss_ceil(vocab - (p.pieces - 1L) * p.piece, wtile);
+            const long whole = loss_best_splits(mtiles * (p.piece / wtile), steps, 256, element), end = loss_best_splits(mtiles * last, steps, 256, element);
+            if (whole > 1 && p.pieces > 1) p.share_rows = whole * p.piece;
+            if (end > 1 && end * last * wtile > p.share_rows) p.share_rows = end * last * wtile;
+            if (p.share_rows) p.share = take(4 * (size_t)p.share_rows * p.dimp);
         }
     }
     p.total = at;

@@ -8,7 +8,8 @@ import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2506_15976_amd", "csrc")
-FIELDS = ("live", "counts", "rank", "order", "targets", "lse2", "down", "both", "own", "part", "x", "w", "g", "acc", "share", "total")
+NUMBERS = ("dimp", "rows", "few", "copy_weight", "piece", "pieces", "part_room", "acc_rows", "share_rows")
+FIELDS = ("choice", "counts", "rank", "order", "targets", "lse2", "down", "both", "own", "part", "x", "w", "g", "acc", "share", "total")
 
 
 @pytest.fixture(scope="module")
@@ -18,19 +19,18 @@ def plan(tmp_path_factory):
     src.write_text('#include "lbscan_loss_plan.h"\n'
                    'extern "C" void plan(long t, int v, int d, int e, int al, int b, int dx, int dw, long* o) {\n'
                    '  const lbscan::LossPlan p = lbscan::loss_plan_of(t, v, d, e, al, b, dx, dw);\n'
-                   '  const long n[] = {p.dimp, p.rows, p.few, p.copy_weight, p.piece, p.pieces, p.chunk, p.chunks, p.splits_x, p.splits_w};\n'
-                   '  for (int i = 0; i < 10; ++i) o[i] = n[i];\n'
+                   f'  const long n[] = {{{", ".join("p." + f for f in NUMBERS)}}};\n'
+                   f'  for (int i = 0; i < {len(NUMBERS)}; ++i) o[i] = n[i];\n'
                    f'  const size_t at[] = {{{", ".join("p." + f for f in FIELDS)}}};\n'
-                   f'  for (int i = 0; i < {len(FIELDS)}; ++i) o[10 + i] = at[i];\n}}\n')
+                   f'  for (int i = 0; i < {len(FIELDS)}; ++i) o[{len(NUMBERS)} + i] = at[i];\n}}\n')
     so = at / "plan.so"
     subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-O1", "-I", CSRC, str(src), "-o", str(so)], check=True)
     lib = ctypes.CDLL(str(so))
 
     def call(tokens, vocab, dim, element, aligned, backward, dx=1, dw=1):
-        out = (ctypes.c_long * (10 + len(FIELDS)))()
+        out = (ctypes.c_long * (len(NUMBERS) + len(FIELDS)))()
         lib.plan(ctypes.c_long(tokens), vocab, dim, element, aligned, backward, dx, dw, out)
-        names = ("dimp", "rows", "few", "copy_weight", "piece", "pieces", "chunk", "chunks", "splits_x", "splits_w") + FIELDS
-        return dict(zip(names, out))
+        return dict(zip(NUMBERS + FIELDS, out))
     return call
 
 
@@ -41,7 +41,7 @@ def test_sizes_and_scratch(plan):
         T, V, D, e = log(0, 24), log(0, 20), log(0, 16), rng.choice([2, 4])
         aligned, backward, dx, dw = (rng.randrange(2) for _ in range(4))
         p = plan(T, V, D, e, aligned, backward, dx, dw)
-        tile = 64 if p["few"] else 256
+        tile = 64 if p["few"] else 256 if e == 2 else 128
         assert p["dimp"] % (64 // e) == 0 and 0 <= p["dimp"] - D < 64 // e
         assert p["rows"] % tile == 0 and 0 <= p["rows"] - T < tile
         assert p["copy_weight"] == int(not aligned or D % (64 // e) != 0)
@@ -49,20 +49,21 @@ def test_sizes_and_scratch(plan):
         assert p["piece"] % 256 == 0 and (p["pieces"] - 1) * p["piece"] < V <= p["pieces"] * p["piece"]
         assert p["piece"] * e * 256 < 1 << 32 and p["dimp"] * e * 256 < 1 << 32
         assert p["rows"] * p["piece"] * e <= max(1 << 30, p["rows"] * 256 * e)
-        vtiles = -(-V // (128 if p["few"] else 256))
-        assert (p["chunks"] - 1) * p["chunk"] < vtiles <= p["chunks"] * p["chunk"]
-        used = {"live": 4, "counts": 4 * -(-T // 1024), "rank": 4 * T, "order": 4 * p["rows"], "targets": 4 * p["rows"],
+        # room for one part of every sum at the least
+        assert backward or p["part_room"] >= p["rows"]
+        assert not (backward and dx) or p["acc_rows"] >= p["rows"]
+        used = {"choice": 32, "counts": 4 * -(-T // 1024), "rank": 4 * T, "order": 4 * p["rows"], "targets": 4 * p["rows"],
                 "x": p["rows"] * p["dimp"] * e}
         if p["copy_weight"]:
             used["w"] = V * p["dimp"] * e
         if backward:
             used.update({k: 4 * p["rows"] for k in ("lse2", "down", "both")}, g=p["rows"] * p["piece"] * e)
             if dx:
-                used["acc"] = 4 * p["splits_x"] * p["rows"] * p["dimp"]
-            if dw and p["splits_w"] > 1:
-                used["share"] = 4 * p["splits_w"] * p["piece"] * p["dimp"]
+                used["acc"] = 4 * p["acc_rows"] * p["dimp"]
+            if dw and p["share_rows"]:
+                used["share"] = 4 * p["share_rows"] * p["dimp"]
         else:
-            used.update(own=4 * p["rows"], part=8 * p["rows"] * p["chunks"])
+            used.update(own=4 * p["rows"], part=8 * p["part_room"])
         at = sorted((p[k], k) for k in used)
         for (a, k), (b, _) in zip(at, at[1:] + [(p["total"], "")]):
             assert a % 256 == 0 and a + used[k] <= b, (k, T, V, D)
