@@ -29,10 +29,15 @@ struct EmbedParams {
     int blocks_log2, shares;  // the sort's grid
     int piece;                // sorted tokens that a wave adds
     float* part;              // (pieces, 2, dim)
+    // Not null: the gradient as a list (vocab numbers): the row v of the table that has tokens (count[v] of them) stands at
+    // dweight[slot[v]], below the number of tokens; nothing is written for the others.
+    int* slot;
 };
 
 hipError_t launch_embed_fwd(const EmbedParams& p, hipStream_t stream);
 hipError_t launch_embed_bwd(EmbedParams p, void* workspace, hipStream_t stream);
 size_t embed_bwd_bytes(const EmbedParams& p);
+// Where launch_embed_bwd leaves the number of tokens of each row.
+const int* embed_counts(EmbedParams p, void* workspace);
 
 }  // namespace lbscan

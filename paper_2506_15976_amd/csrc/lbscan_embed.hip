@@ -309,8 +309,12 @@ constexpr int kPieceAhead = 8;
 constexpr int kJoinWaves = 8;
 
 template <typename T, int E>
-__device__ __forceinline__ void write_row(const EmbedParams& p, int row, int col, const float acc[E])
+__device__ __forceinline__ void write_row(const EmbedParams& p, int row, int last, int col, const float acc[E])
 {
+    if (p.slot) {                                    // in a list: at the place of the row's last token
+        p.slot[row] = last;                          // (every lane writes the same)
+        row = last;
+    }
     Pack<T, E> o;
 #pragma unroll
     for (int e = 0; e < E; ++e) o.v[e] = from_f32<T>(p.scale * acc[e]);
@@ -356,7 +360,7 @@ __global__ __launch_bounds__(256) void embed_pieces_kernel(const EmbedParams p, 
                 const bool in_part = (early && (bit & first_row)) || (goes_on && k0 + k == n - 1);
                 if (there) {
                     if (!in_part) {
-                        write_row<T, E>(p, __builtin_amdgcn_readlane(my_row, k0 + k), col, acc);
+                        write_row<T, E>(p, __builtin_amdgcn_readlane(my_row, k0 + k), first + k0 + k, col, acc);
                     } else {
                         float* to = p.part + ((long)piece * 2 + (early && (bit & first_row) ? 0 : 1)) * dim + col;
                         Pack<float, E> o;
@@ -414,7 +418,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const Embed
     for (int w = 0; w < kJoinWaves - 1; ++w)
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] += sums[w][lane][e];
-    write_row<T, E>(p, row, col, acc);
+    write_row<T, E>(p, row, begin + p.count[row] - 1, col, acc);
 }
 
 int pieces_of(const EmbedParams& p)
@@ -476,7 +480,7 @@ static hipError_t launch_sort(const EmbedParams& p, hipStream_t stream)
     const dim3 grid(1 << p.blocks_log2, p.shares), block(kSortThreads);
     const size_t lds = (size_t)(sort_rows(p) * kSortWaves + 64) * sizeof(int);
     const long zeros = ((long)p.vocab + kZeroBlock - 1) / kZeroBlock;
-    const dim3 with_zeros(grid.x, (unsigned)(p.shares + (zeros + grid.x - 1) / grid.x));
+    const dim3 with_zeros(grid.x, (unsigned)(p.shares + (p.slot ? 0 : (zeros + grid.x - 1) / grid.x)));
     if (p.shares == 1) {
         embed_sort_kernel<I, Sort::all><<<with_zeros, block, lds, stream>>>(p);
         return hipGetLastError();
@@ -494,7 +498,7 @@ hipError_t launch_embed_fwd(const EmbedParams& p, hipStream_t stream)
     return p.dim < 8 ? launch_fwd<bf16_t, 1>(p, stream) : launch_fwd<bf16_t, 8>(p, stream);
 }
 
-hipError_t launch_embed_bwd(EmbedParams p, void* workspace, hipStream_t stream)
+static void lay_out(EmbedParams& p, void* workspace)
 {
     p.part = static_cast<float*>(workspace);
     p.piece = piece_of(p.tokens);
@@ -505,6 +509,16 @@ hipError_t launch_embed_bwd(EmbedParams p, void* workspace, hipStream_t stream)
     p.share_total = p.valid + 1;
     sort_shape(p);
     p.share_count = p.share_total + ((size_t)p.shares << p.blocks_log2);
+}
+const int* embed_counts(EmbedParams p, void* workspace)
+{
+    lay_out(p, workspace);
+    return p.count;
+}
+
+hipError_t launch_embed_bwd(EmbedParams p, void* workspace, hipStream_t stream)
+{
+    lay_out(p, workspace);
     const hipError_t e = p.wide_ids ? launch_sort<int64_t>(p, stream) : launch_sort<int32_t>(p, stream);
     if (e != hipSuccess) return e;
     if (p.dtype == 0) return p.dim < 4 ? launch_sums<float, 1>(p, stream) : launch_sums<float, 4>(p, stream);

@@ -3,6 +3,11 @@
 //     lse_t = log sum_v exp l_tv        loss_t = lse_t - l_t,target(t)
 //     G_tv = (g_t + e_t) exp(l_tv - lse_t) - g_t [v = target(t)],   g, e: gradients of loss and lse
 //     dx_t = scale sum_v G_tv W_v       dW_v = scale sum_t G_tv x_t
+// In bf16 G is rounded.  The many small terms' roundings are no more than that of the result; the targets' are most of
+// the gradient, and what is left of them, rest_t = G_t,target(t) - bf16(G_t,target(t)), is added by itself:
+//     dx_t += scale rest_t W_target(t)  dW_v += scale sum of rest_t x_t over the tokens t with target v
+// (2-norm of the error of dx and dweight over that of the result, 16384 x 50000 x 768: 2.4e-3 without, 1.7e-3 with, of which
+// their own rounding is 1.66e-3).
 // Tokens whose target is no row of the table are left out of all of it: the others (the live ones) are packed together first.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -34,7 +39,10 @@ struct LossTiles {
     const void* x;                    // (rows, dimp): the live rows, then zeros to a whole tile
     void* g;                          // (rows, piece)
     const int* targets;               // (rows)
-    const float *lse2, *down, *both;  // (rows) lse log2(e), g, g + e; zeros behind the live ones
+    const float *lse2, *both;         // (rows) lse log2(e), g + e
+    const float* down;                // (rows) fp32: g; bf16: the rounded slope at the target
+    const int *tokens_of, *slot;      // bf16, dweight: tokens of each row of the table, and its place in the list
+    const void* list;                 // (.., dimp) sums of rest_t x_t
     float* own;                       // (rows) l of the target
     float2* part;                     // (chunks, live rows) maximum and sum of a chunk of the vocabulary
     float* acc;                       // (splits, live rows, dimp)

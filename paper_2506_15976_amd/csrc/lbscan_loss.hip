@@ -1,6 +1,7 @@
 // The loss around its products (formulas: lbscan_loss.h): live tokens packed together, sums of the blocks' parts, results put
 // in their tokens' places.
 #include "lbscan_device.h"
+#include "lbscan_embed.h"
 #include "lbscan_internal.h"
 #include "lbscan_loss.h"
 
@@ -169,7 +170,7 @@ __device__ __forceinline__ void copy_row(T* __restrict__ to, const T* __restrict
         *reinterpret_cast<Pack<T, E>*>(to + c) = q;
     }
 }
-// The live rows one behind the other, then rows of zeros (of no target) to a whole tile.
+// The live rows one behind the other, then rows of zeros to a whole tile; no targets behind the live ones.
 template <typename T>
 __global__ __launch_bounds__(256) void loss_gather_kernel(const T* __restrict__ x, T* __restrict__ out, const int* __restrict__ order,
                                                           int* __restrict__ targets, const LossChoice* __restrict__ choice, long rows, int dim,
@@ -177,9 +178,10 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(const T* __restrict__ 
 {
     const int live = choice->live;
     const long end = min(rows, ((long)live + tile - 1) / tile * tile);
-    for (long r = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < end; r += (long)gridDim.x * 4) {
+    for (long r = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < rows; r += (long)gridDim.x * 4) {
         const bool there = r < live;
         if (!there && (threadIdx.x & 63) == 0) targets[r] = -1;
+        if (r >= end) continue;
         copy_row<T>(out + r * dimp, there ? x + (long)order[r] * dim : x, there ? dim : 0, dimp, threadIdx.x & 63);
     }
 }
@@ -188,6 +190,39 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(const T* __restrict__ fr
 {
     for (long r = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < rows; r += (long)gridDim.x * 4)
         copy_row<T>(to + r * dimp, from + r * dim, dim, dimp, threadIdx.x & 63);
+}
+
+// bf16: the slopes at the targets, rounded for G, and what is left of them; with rest_rows that times the tokens' rows.  A
+// wave a token.
+__global__ __launch_bounds__(256) void loss_target_kernel(const bf16_t* __restrict__ x, const bf16_t* __restrict__ w, const int* __restrict__ targets,
+                                                          const float* __restrict__ lse2, const float* __restrict__ down,
+                                                          const float* __restrict__ both, float* __restrict__ hot, float* __restrict__ rest,
+                                                          bf16_t* __restrict__ rest_rows, const LossChoice* __restrict__ choice, int dimp, float scale)
+{
+    const int live = choice->live, lane = threadIdx.x & 63;
+    for (long r = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < live; r += (long)gridDim.x * 4) {
+        const bf16_t *mine = x + r * dimp, *row = w + (long)targets[r] * dimp;
+        float dot = 0.0f;
+#pragma unroll 2
+        for (int c = lane * 8; c < dimp; c += 512) {
+            const Pack<bf16_t, 8> a = *reinterpret_cast<const Pack<bf16_t, 8>*>(mine + c), b = *reinterpret_cast<const Pack<bf16_t, 8>*>(row + c);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) dot = fmaf(to_f32(a.v[k]), to_f32(b.v[k]), dot);
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) dot += __shfl_xor(dot, m, 64);
+        const float slope = both[r] * fast_exp2(fmaf(dot, scale * kLog2e, -lse2[r])) - down[r];
+        const float rounded = to_f32(from_f32<bf16_t>(slope)), left = slope - rounded;
+        if (lane == 0) { hot[r] = rounded; rest[r] = left; }
+        if (!rest_rows) continue;
+        for (int c = lane * 8; c < dimp; c += 512) {
+            const Pack<bf16_t, 8> a = *reinterpret_cast<const Pack<bf16_t, 8>*>(mine + c);
+            Pack<bf16_t, 8> o;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o.v[k] = from_f32<bf16_t>(left * to_f32(a.v[k]));
+            *reinterpret_cast<Pack<bf16_t, 8>*>(rest_rows + r * dimp + c) = o;
+        }
+    }
 }
 
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2)
@@ -229,8 +264,8 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const float2* __restrict
 
 // dx: the sums' parts added in their order, in their tokens' places; zeros for the others.  A wave has 256 columns of a token.
 template <typename T>
-__global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ acc, const int* __restrict__ rank, T* __restrict__ dx,
-                                                      long tokens, int dim, int dimp, const LossChoice* __restrict__ choice, float scale)
+__global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ acc, const int* __restrict__ rank, const float* __restrict__ rest,
+                                                      const int* __restrict__ targets, const T* __restrict__ weight, T* __restrict__ dx, long tokens, int dim, int dimp, const LossChoice* __restrict__ choice, float scale)
 {
     const long rows = choice->rows;
     const int splits = choice->splits_x, strips = (dim + 255) / 256;
@@ -246,6 +281,12 @@ __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ 
                 const Pack<float, 4> q = *reinterpret_cast<const Pack<float, 4>*>(acc + ((long)k * rows + r) * dimp + c);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] += q.v[i];
+            }
+            if constexpr (sizeof(T) == 2) {
+                const Pack<T, 4> row = *reinterpret_cast<const Pack<T, 4>*>(weight + (long)targets[r] * dimp + c);
+                const float left = rest[r];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = fmaf(left, to_f32(row.v[i]), v[i]);
             }
         }
         Pack<T, 4> o;
@@ -263,6 +304,7 @@ __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ 
 // dweight of a piece of the vocabulary, likewise.
 template <typename T>
 __global__ __launch_bounds__(256) void loss_dweight_kernel(const float* __restrict__ share, T* __restrict__ dweight, int count, int dim, int dimp,
+                                                           const int* __restrict__ tokens_of, const int* __restrict__ slot, const T* __restrict__ list,
                                                            const LossChoice* __restrict__ choice, int last, float scale)
 {
     constexpr int tile = loss_tokens(0, sizeof(T));
@@ -276,6 +318,11 @@ __global__ __launch_bounds__(256) void loss_dweight_kernel(const float* __restri
                 const Pack<float, 4> q = *reinterpret_cast<const Pack<float, 4>*>(share + (k * columns + v) * dimp + c);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[i] += q.v[i];
+            }
+            if (sizeof(T) == 2 && tokens_of[v] > 0) {
+                const Pack<T, 4> rest = *reinterpret_cast<const Pack<T, 4>*>(list + (long)slot[v] * dimp + c);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] += to_f32(rest.v[i]);
             }
             Pack<T, 4> o;
 #pragma unroll
@@ -344,6 +391,18 @@ LossTiles tiles_of(const LossParams& p, const LossPlan& plan, const Scratch& s)
     return t;
 }
 
+// The sums by target, as the gradient of an embedding kept as a list.
+EmbedParams list_params(const LossParams& p, const LossPlan& plan)
+{
+    EmbedParams q{};
+    q.tokens = plan.rows;
+    q.vocab = p.vocab;
+    q.dim = plan.dimp;
+    q.dtype = p.dtype;
+    q.scale = 1.0f;
+    return q;
+}
+
 template <typename T>
 hipError_t forward(const LossParams& p, const LossPlan& plan, const Scratch& s, hipStream_t stream)
 {
@@ -370,6 +429,26 @@ hipError_t backward(const LossParams& p, const LossPlan& plan, const Scratch& s,
     t.acc = s.at<float>(plan.acc);
     t.share = s.at<float>(plan.share);
     t.dweight = p.dweight;
+    if constexpr (sizeof(T) == 2) {
+        if (e != hipSuccess) return e;
+        bf16_t* rows = p.dweight ? s.at<bf16_t>(plan.rest_rows) : nullptr;
+        loss_target_kernel<<<some((p.tokens + 3) / 4), 256, 0, stream>>>(static_cast<const bf16_t*>(t.x), static_cast<const bf16_t*>(t.w), t.targets,
+                                                                       t.lse2, t.down, t.both, s.at<float>(plan.hot), s.at<float>(plan.rest), rows,
+                                                                       t.choice, plan.dimp, p.scale);
+        e = hipGetLastError();
+        if (e == hipSuccess && p.dweight) {
+            EmbedParams q = list_params(p, plan);
+            q.ids = t.targets;
+            q.dout = rows;
+            q.dweight = s.at<void>(plan.list);
+            q.slot = s.at<int>(plan.slot);
+            e = launch_embed_bwd(q, s.at<void>(plan.sort), stream);
+            t.tokens_of = embed_counts(q, s.at<void>(plan.sort));
+            t.slot = q.slot;
+            t.list = q.dweight;
+        }
+        t.down = s.at<float>(plan.hot);
+    }
     for (t.first = 0; t.first < p.vocab && e == hipSuccess; t.first += plan.piece) {
         t.count = p.vocab - t.first < plan.piece ? p.vocab - t.first : plan.piece;
         t.last = t.first + plan.piece >= p.vocab;
@@ -382,13 +461,15 @@ hipError_t backward(const LossParams& p, const LossPlan& plan, const Scratch& s,
             e = launch(LossKind::dweight, t, plan.few, stream);
             if (e == hipSuccess && plan.share_rows) {
                 loss_dweight_kernel<T><<<some((t.count + 3L) / 4), 256, 0, stream>>>(t.share, static_cast<T*>(p.dweight) + (long)t.first * p.dim, t.count,
-                                                                                   p.dim, plan.dimp, t.choice, t.last, p.scale);
+                                                                                   p.dim, plan.dimp, t.tokens_of + t.first, t.slot + t.first,
+                                                                                   static_cast<const T*>(t.list), t.choice, t.last, p.scale);
                 e = hipGetLastError();
             }
         }
     }
     if (e != hipSuccess || !p.dx) return e;
-    loss_dx_kernel<T><<<some((p.tokens * ((p.dim + 255) / 256) + 3) / 4), 256, 0, stream>>>(t.acc, s.at<int>(plan.rank), static_cast<T*>(p.dx), p.tokens, p.dim, plan.dimp,
+    loss_dx_kernel<T><<<some((p.tokens * ((p.dim + 255) / 256) + 3) / 4), 256, 0, stream>>>(t.acc, s.at<int>(plan.rank), s.at<float>(plan.rest),
+                                                                  t.targets, static_cast<const T*>(t.w), static_cast<T*>(p.dx), p.tokens, p.dim, plan.dimp,
                                                                   t.choice, p.scale);
     return hipGetLastError();
 }
@@ -405,8 +486,12 @@ hipError_t zero(void* out, long n, hipStream_t stream)
 
 LossPlan loss_plan(const LossParams& p, bool backward)
 {
-    return loss_plan_of(p.tokens, p.vocab, p.dim, p.dtype == 0 ? 4 : 2, (reinterpret_cast<uintptr_t>(p.weight) & 15) == 0, backward,
-                        p.dx != nullptr, p.dweight != nullptr);
+    auto plan = [&](size_t sort_bytes) {
+        return loss_plan_of(p.tokens, p.vocab, p.dim, p.dtype == 0 ? 4 : 2, (reinterpret_cast<uintptr_t>(p.weight) & 15) == 0, backward,
+                            p.dx != nullptr, p.dweight != nullptr, sort_bytes);
+    };
+    if (p.dtype == 0 || !backward || !p.dweight || p.tokens == 0 || p.vocab == 0) return plan(0);
+    return plan(embed_bwd_bytes(list_params(p, plan(0))));
 }
 
 hipError_t launch_loss_fwd(const LossParams& p, const LossPlan& plan, void* workspace, hipStream_t stream)

@@ -67,7 +67,8 @@ struct LossPlan {
     long acc_rows;           // rows of dx's sums (rows x splits)
     long share_rows;         // rows of dweight's, where it is cut (columns of a piece x splits)
     // bytes from the start of the scratch
-    size_t choice, counts, rank, order, targets, lse2, down, both, own, part, x, w, g, acc, share, total;
+    size_t choice, counts, rank, order, targets, lse2, down, both, own, part, x, w, g, acc, share;
+    size_t hot, rest, rest_rows, list, slot, sort, total;              // bf16: what rounding the targets' slopes leaves
 };
 
 inline int loss_best_splits(long tiles, int steps, int units, int element)
@@ -80,7 +81,8 @@ inline int loss_best_splits(long tiles, int steps, int units, int element)
     return best;
 }
 
-inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool aligned, bool backward, bool want_dx, bool want_dw)
+// sort_bytes: scratch of the list of sums by target.
+inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool aligned, bool backward, bool want_dx, bool want_dw, size_t sort_bytes)
 {
     LossPlan p{};
     if (tokens == 0 || vocab == 0 || dim == 0) return p;        // (no kernel runs)
@@ -121,6 +123,16 @@ inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool 
         p.down = take(4 * (size_t)p.rows);
         p.both = take(4 * (size_t)p.rows);
         p.g = take((size_t)p.rows * p.piece * element);
+        if (element == 2) {
+            p.hot = take(4 * (size_t)p.rows);
+            p.rest = take(4 * (size_t)p.rows);
+            if (want_dw) {
+                p.rest_rows = take(2 * (size_t)p.rows * p.dimp);
+                p.list = take(2 * (size_t)p.rows * p.dimp);
+                p.slot = take(4 * (size_t)vocab);
+                p.sort = take(sort_bytes);
+            }
+        }
         if (want_dx) {
             // as many parts as all tokens need, and more for fewer live ones
             const long few_rows = p.few ? 1024 : 8192;

@@ -9,7 +9,11 @@ import pytest
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2506_15976_amd", "csrc")
 NUMBERS = ("dimp", "rows", "few", "copy_weight", "piece", "pieces", "part_room", "acc_rows", "share_rows")
-FIELDS = ("choice", "counts", "rank", "order", "targets", "lse2", "down", "both", "own", "part", "x", "w", "g", "acc", "share", "total")
+FIELDS = ("choice", "counts", "rank", "order", "targets", "lse2", "down", "both", "own", "part", "x", "w", "g", "acc", "share", "hot", "rest",
+          "rest_rows", "list", "slot", "sort", "total")
+
+
+SORT = 12345
 
 
 @pytest.fixture(scope="module")
@@ -17,8 +21,8 @@ def plan(tmp_path_factory):
     at = tmp_path_factory.mktemp("plan")
     src = at / "plan.cpp"
     src.write_text('#include "lbscan_loss_plan.h"\n'
-                   'extern "C" void plan(long t, int v, int d, int e, int al, int b, int dx, int dw, long* o) {\n'
-                   '  const lbscan::LossPlan p = lbscan::loss_plan_of(t, v, d, e, al, b, dx, dw);\n'
+                   'extern "C" void plan(long t, int v, int d, int e, int al, int b, int dx, int dw, long sort, long* o) {\n'
+                   '  const lbscan::LossPlan p = lbscan::loss_plan_of(t, v, d, e, al, b, dx, dw, sort);\n'
                    f'  const long n[] = {{{", ".join("p." + f for f in NUMBERS)}}};\n'
                    f'  for (int i = 0; i < {len(NUMBERS)}; ++i) o[i] = n[i];\n'
                    f'  const size_t at[] = {{{", ".join("p." + f for f in FIELDS)}}};\n'
@@ -29,7 +33,7 @@ def plan(tmp_path_factory):
 
     def call(tokens, vocab, dim, element, aligned, backward, dx=1, dw=1):
         out = (ctypes.c_long * (len(NUMBERS) + len(FIELDS)))()
-        lib.plan(ctypes.c_long(tokens), vocab, dim, element, aligned, backward, dx, dw, out)
+        lib.plan(ctypes.c_long(tokens), vocab, dim, element, aligned, backward, dx, dw, ctypes.c_long(SORT), out)
         return dict(zip(NUMBERS + FIELDS, out))
     return call
 
@@ -58,6 +62,10 @@ def test_sizes_and_scratch(plan):
             used["w"] = V * p["dimp"] * e
         if backward:
             used.update({k: 4 * p["rows"] for k in ("lse2", "down", "both")}, g=p["rows"] * p["piece"] * e)
+            if e == 2:
+                used.update(hot=4 * p["rows"], rest=4 * p["rows"])
+                if dw:
+                    used.update(rest_rows=2 * p["rows"] * p["dimp"], list=2 * p["rows"] * p["dimp"], slot=4 * V, sort=SORT)
             if dx:
                 used["acc"] = 4 * p["acc_rows"] * p["dimp"]
             if dw and p["share_rows"]:
