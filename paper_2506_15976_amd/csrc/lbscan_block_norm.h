@@ -61,11 +61,12 @@ inline BlockNormShape block_norm_shape(const BlockNormParams& p, bool backward)
     if (n <= 16) { s.lanes = 16; return s; }
     // at most 16 elements a lane; in the widest teams 24, which the gradients have registers for without gate and residual only
     // (gradients with a residual hold so much that a compute unit has one block of 16 elements a lane, whose reductions nothing
-    // covers: 8 elements in twice the waves where that makes teams of four and eight.  MI355X, us, gradients, 16 / 8: 8192 x 2048
-    // bf16 with everything 94.9 / 74.9, 4096 x 4096 bf16 without a gate 80.9 / 62.2)
-    const bool narrow = backward && p.with_residual && n > 256 && n <= 1024;
+    // covers: 8 elements in twice the waves where that makes teams of four to sixteen.  MI355X, us, gradients, 16 / 8: 8192 x 2048
+    // bf16 with everything 94.9 / 74.9, 4096 x 4096 bf16 without a gate 80.9 / 62.2, 2048 x 8192 the norm in front alone 71.6 / 59.8;
+    // sixteen waves do not have the registers for a gate)
+    const bool narrow = backward && p.with_residual && n > 256 && n <= (p.gate ? 1024 : 2048);
     const int most = narrow ? 2 : 16 / s.pack;
-    for (s.waves = 1; s.waves <= 8; s.waves *= 2) {
+    for (s.waves = 1; s.waves <= (narrow ? 16 : 8); s.waves *= 2) {
         s.packs = (n + 64 * s.waves - 1) / (64 * s.waves);
         if (s.packs <= most) return s;
     }
@@ -79,7 +80,7 @@ inline int block_norm_teams(const BlockNormShape& s) { return s.packs == 0 || s.
 inline int block_norm_shares(const BlockNormParams& p)
 {
     const BlockNormShape s = block_norm_shape(p, true);
-    const long teams = block_norm_teams(s), whole = (p.rows + teams - 1) / teams, most = s.waves == 8 || s.packs == 0 ? 256 : 512;
+    const long teams = block_norm_teams(s), whole = (p.rows + teams - 1) / teams, most = s.waves >= 8 || s.packs == 0 ? 256 : 512;
     return (int)(whole < most ? whole : most);
 }
 
