@@ -327,7 +327,7 @@ size_t lbscan_embed_workspace_bytes(const lbscan_embed_args *args);
  * s = slots[b] of the pools, or at b without slots.  A row whose slot is outside [0, pool), or that an earlier row has already, is
  * padding: its y is zeros and no state is touched for it. */
 typedef struct lbscan_step_args {
-    int32_t batch, dim, dstate;   /* B, D, N in 1 .. LBSCAN_MAX_DSTATE; B or D may be 0.  B * D < 2^31;
+    int32_t batch, dim, dstate;   /* B, D, N in 1 .. LBSCAN_MAX_DSTATE; B or D may be 0.  B * D <= 2^31 - 4096;
                                      B <= 65536 with slots */
     int32_t pool;                 /* rows of the states; >= B without slots */
     int32_t dtype;                /* storage type of x, delta, z, Bm, Cm, conv_state, y */
@@ -359,7 +359,8 @@ int lbscan_step(const lbscan_step_args *args, void *hip_stream);
  * lengths[b], held to 0 .. L: tokens of row b that are there (a padded batch); y is zero behind them and x is not read, and the
  * state leaves as it is after the last of them.  slots and pool as in lbscan_step; a row of padding has zeros in y. */
 typedef struct lbscan_conv_state_args {
-    int32_t batch, dim, seqlen;   /* B, D, L; any may be 0 (the state stays).  D * L < 2^31; B <= 65536 with slots */
+    int32_t batch, dim, seqlen;   /* B, D, L; any may be 0 (the state stays).  D * L <= 2^31 - 4096; B <= 65536 with
+                                     slots */
     int32_t width;                /* K, 1..4 */
     int32_t pool;                 /* rows of the state; >= B without slots */
     int32_t dtype;                /* storage type of x, state, y */

@@ -25,6 +25,8 @@ bool enough(const void* workspace, size_t have, size_t need)
 }
 int done(hipError_t e, const char* where) { return e == hipSuccess ? LBSCAN_OK : hip_fail(e, where); }
 
+// Values of a row of x: whole blocks of a row's end still count in 32 bits.
+constexpr int64_t kMostValues = 0x7fffffff - 4095;
 constexpr int kMostSlots = 65536;             // rows of a batch whose slots each row looks through
 
 // Rows of the batch and of the pools.
@@ -100,7 +102,7 @@ int lbscan_step(const lbscan_step_args* a, void* hip_stream)
     if (a->batch < 0 || a->dim < 0 || a->dstate < 0 || a->conv_width < 0) return LBSCAN_EINVAL;
     if (!known_type(a->dtype)) return LBSCAN_EUNSUPPORTED;
     if (!is_flag(a->delta_softplus) || !is_flag(a->conv_activation)) return LBSCAN_EINVAL;
-    if (a->conv_width > 4 || (int64_t)a->batch * a->dim > 0x7fffffff) return LBSCAN_EUNSUPPORTED;
+    if (a->conv_width > 4 || (int64_t)a->batch * a->dim > kMostValues) return LBSCAN_EUNSUPPORTED;
     const int rc = check_pool(a->batch, a->pool, a->slots);
     if (rc != LBSCAN_OK) return rc;
     if (a->batch == 0 || a->dim == 0) return LBSCAN_OK;
@@ -136,7 +138,7 @@ int lbscan_conv1d_prompt(const lbscan_conv_state_args* a, void* hip_stream)
     if (a->batch < 0 || a->dim < 0 || a->seqlen < 0) return LBSCAN_EINVAL;
     if (!known_type(a->dtype) || a->width < 1 || a->width > 4) return LBSCAN_EUNSUPPORTED;
     if (!is_flag(a->activation)) return LBSCAN_EINVAL;
-    if ((int64_t)a->dim * a->seqlen > 0x7fffffff) return LBSCAN_EUNSUPPORTED;
+    if ((int64_t)a->dim * a->seqlen > kMostValues) return LBSCAN_EUNSUPPORTED;
     const int rc = check_pool(a->batch, a->pool, a->slots);
     if (rc != LBSCAN_OK) return rc;
     if (a->batch == 0 || a->dim == 0 || a->seqlen == 0) return LBSCAN_OK;

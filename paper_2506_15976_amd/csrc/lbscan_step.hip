@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256) void prompt_kernel(const PromptParams p, unsig
         if ((unsigned)slot >= (unsigned)p.pool || (p.slots && taken(p.slots, b, slot))) slot = -1;
         const int n = slot < 0 ? 0 : p.lengths ? min(max(p.lengths[b], 0), L) : L;
         const T* x = static_cast<const T*>(p.x) + b * p.x_stride + (long)d * L;
-        const bool whole = there && t0 + E <= n;              // all tokens are there
+        const bool whole = there && t0 <= n - E;              // all tokens are there
         Pack<T, E> own{};
         if (whole) own = *reinterpret_cast<const Pack<T, E>*>(x + t0);
         else if (there && t0 < n) {
@@ -258,7 +258,7 @@ __global__ __launch_bounds__(256) void prompt_kernel(const PromptParams p, unsig
 #pragma unroll
             for (int e = 0; e < E; ++e) out.v[e] = value(e);
             *reinterpret_cast<Pack<T, E>*>(y) = out;
-        } else if (t0 >= n && t0 + E <= L) {
+        } else if (t0 >= n && t0 <= L - E) {
             *reinterpret_cast<Pack<T, E>*>(y) = Pack<T, E>{};
         } else {
 #pragma unroll

@@ -141,12 +141,35 @@ inline void set_python_error(const Failure& e)
     PyErr_SetObject(type.ptr(), type(e.code, e.what()).ptr());
 }
 
+// A backward pass that is being recorded into a graph, and whose next node adds up a leaf's gradient on the default stream, where
+// an eager graph that still lives has left it: torch would make the default stream wait for the recorded one, which ends
+// the recording, or the process, from a thread that no caller sees.
+inline void refuse_leaves_of_the_default_stream()
+{
+    const auto node = torch::autograd::get_current_node();
+    if (!node) return;
+    for (const auto& edge : node->next_edges()) {
+        if (!edge.function) continue;
+        const auto leaf = edge.function->stream();
+        if (!leaf || leaf->device_type() != c10::DeviceType::CUDA) continue;
+        const c10::impl::VirtualGuardImpl guard(leaf->device_type());
+        hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+        if (*leaf != guard.getDefaultStream(leaf->device()) || *leaf == guard.getStream(leaf->device()) ||
+            hipStreamIsCapturing(c10::hip::getCurrentHIPStream(leaf->device_index()).stream(), &status) != hipSuccess)
+            continue;
+        if (status == hipStreamCaptureStatusActive)
+            throw Failure(LBSCAN_EUNSUPPORTED, "a backward pass cannot be captured while an eager graph of the same leaves, made on the "
+                                               "default stream, lives: delete its outputs first");
+    }
+}
+
 // A node's backward pass.  Its errors cross torch's threads, which hand Python errors on as they are and make a RuntimeError
 // of every other exception.
 template <typename F>
 variable_list backward_pass(const F& pass)
 {
     try {
+        refuse_leaves_of_the_default_stream();
         return pass();
     } catch (const Failure& e) {
         const py::gil_scoped_acquire gil;

@@ -17,11 +17,19 @@ int64_t expect_rows(const char* name, const Tensor& t, int64_t B, int64_t n, at:
     return dense || B <= 1 ? 0 : t.stride(0);
 }
 
-// An output of the caller's must not be one of the inputs.
+// An output of the caller's must not have memory of an input, which other blocks may still have to read.
+std::pair<uintptr_t, uintptr_t> extent(const Tensor& t)
+{
+    int64_t last = 0;
+    for (int64_t k = 0; k < t.dim(); ++k) last += (t.size(k) - 1) * t.stride(k);
+    const auto first = reinterpret_cast<uintptr_t>(t.data_ptr());
+    return {first, first + (last + 1) * t.element_size()};
+}
 void expect_apart(const Maybe& out, const Maybe& input, const char* name)
 {
-    if (out && input && out->numel() && out->data_ptr() == input->data_ptr())
-        throw Failure(LBSCAN_EINVAL, std::string("out must not be ") + name);
+    if (!out || !input || !out->numel() || !input->numel()) return;
+    const auto a = extent(*out), b = extent(*input);
+    if (a.first < b.second && b.first < a.second) throw Failure(LBSCAN_EINVAL, std::string("out must not be, or share memory with, ") + name);
 }
 
 // A pool of states, and the rows' places in it.
@@ -76,9 +84,14 @@ Tensor step(Tensor x, Tensor delta, Tensor A, Tensor Bm, Tensor Cm, Tensor state
     const Stream stream(stream_object, x);
     expect("out", out, {B, D}, type, x);
     expect_writable("out", out);
-    expect_apart(out, x, "x");
-    expect_apart(out, delta, "delta");
-    expect_apart(out, z, "z");
+    if (out) {
+        using Named = std::pair<const Maybe, const char*>;
+        for (const auto& [t, name] : {Named{x, "x"}, Named{delta, "delta"}, Named{z, "z"}, Named{Bm, "Bm"}, Named{Cm, "Cm"}, Named{A, "A"},
+                                      Named{state, "state"}, Named{conv_state, "conv_state"}, Named{Dskip, "Dskip"},
+                                      Named{delta_bias, "delta_bias"}, Named{conv_weight, "conv_weight"}, Named{conv_bias, "conv_bias"},
+                                      Named{slots, "slots"}})
+            expect_apart(out, t, name);
+    }
     Tensor y = out ? *out : fresh(stream, {B, D}, x, type);
     a.batch = size32("x", B);
     a.dim = size32("x", D);
@@ -127,6 +140,11 @@ Tensor conv1d_prompt(Tensor x, Maybe state, Tensor weight, Maybe bias, bool acti
     expect("out", out, x.sizes(), type, x);
     expect_writable("out", out);
     expect_apart(out, x, "x");
+    expect_apart(out, state, "state");
+    expect_apart(out, weight, "weight");
+    expect_apart(out, bias, "bias");
+    expect_apart(out, lengths, "lengths");
+    expect_apart(out, slots, "slots");
     Tensor y = out ? *out : fresh(stream, x.sizes(), x, type);
     a.batch = size32("x", B);
     a.dim = size32("x", D);
@@ -192,6 +210,8 @@ BlockNormResult block_norm_run(const BlockNorm& n, bool stats, const Maybe& out,
     expect_apart(out, x, "x");
     expect_apart(out, n.gate, "the gate");
     expect_apart(out, n.residual, "the residual");
+    expect_apart(out, n.weight, "weight");
+    expect_apart(out, n.branch_weight, "branch_weight");
     BlockNormResult r;
     r.y = out ? *out : fresh(stream, x.sizes(), x, x.scalar_type());
     if (n.residual) r.sum = fresh(stream, x.sizes(), x, at::kFloat);

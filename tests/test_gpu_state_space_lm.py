@@ -126,3 +126,40 @@ def test_a_pool_says_what_whole_sequences_say(example):
     enter([5, 6, 7], [5, 3, 8], [0, 3, 5])                        # (slot 0 was row 1's)
     for rows in ([0, 2, 3, 4, 5, 6], [7, 6, 5, 4, 3, 2], [7], [0, 5]):
         go_on(rows)
+
+
+# Gradients that the convolution and the scan add up with one fp32 atomic a wave or block, in any order: of 150 tokens' terms at
+# most 20 such sums a value, each rounded by 2^-24 of the terms' sizes S at most, so two runs differ by at most 40 * 2^-24 S.  150
+# terms of either sign add to about S / 12; the largest of a tensor's sums is at least a third of that: 36 * 40 * 2^-24 = 9e-5.
+ANY_ORDER = ("conv", "conv_bias", "A", "skip", "dt_bias")
+
+
+def test_captured_training_steps(example):
+    """Loss and gradients of the model from a graph, replayed with other documents between eager work: as eager steps."""
+    model = example.StateSpaceLM(37, 48, 2, dtype=torch.bfloat16)
+    g = torch.Generator().manual_seed(3)
+    ids, targets = (t.cuda() for t in example.documents(5, 30, 37, g))
+    leaves = list(model.parameters.values())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.autograd.grad(model.loss(ids, targets), leaves)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss = model.loss(ids, targets)
+        grads = torch.autograd.grad(loss, leaves)
+    loss = loss.detach()
+    for _ in range(4):
+        for t, new in zip((ids, targets), example.documents(5, 30, 37, g)):
+            t.copy_(new)
+        graph.replay()
+        want = model.loss(ids, targets)
+        others = torch.autograd.grad(want, leaves)
+        torch.cuda.synchronize()
+        assert torch.equal(loss, want.detach())
+        for a, b, k in zip(grads, others, model.parameters):
+            if k.rstrip("01") in ANY_ORDER:
+                assert float((a - b).abs().max()) <= 1e-4 * float(b.abs().max()), k
+            else:
+                assert torch.equal(a, b), k

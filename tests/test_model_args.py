@@ -63,7 +63,7 @@ def test_struct_layouts():
     (dict(batch=-1), EINVAL), (dict(dim=-1), EINVAL), (dict(dstate=-1), EINVAL), (dict(conv_width=-1), EINVAL),
     (dict(dtype=2), EUNSUPPORTED), (dict(delta_softplus=2), EINVAL), (dict(conv_activation=-1), EINVAL),
     (dict(conv_width=5), EUNSUPPORTED), (dict(dstate=17), EUNSUPPORTED), (dict(dstate=0), EUNSUPPORTED),
-    (dict(batch=1 << 16, dim=1 << 16, pool=1 << 16), EUNSUPPORTED), (dict(pool=1), EINVAL), (dict(pool=-1, slots=P), EINVAL),
+    (dict(batch=1 << 16, dim=1 << 16, pool=1 << 16), EUNSUPPORTED), (dict(batch=1, dim=(1 << 31) - 4095), EUNSUPPORTED), (dict(pool=1), EINVAL), (dict(pool=-1, slots=P), EINVAL),
     (dict(slots=P + 2), EINVAL), (dict(batch=65537, pool=70000, slots=P), EUNSUPPORTED),
     *[(dict([(name, None)]), EINVAL) for name in ("x", "delta", "Bm", "Cm", "A", "state", "y", "conv_weight", "conv_state")],
     *[(dict([(name, P + 2)]), EINVAL) for name in ("x", "z", "A", "Dskip", "delta_bias", "conv_weight", "conv_bias", "state", "y")],
@@ -78,7 +78,8 @@ def test_step_refuses(lib, fields, code):
 @pytest.mark.parametrize("fields,code", [
     (dict(batch=-1), EINVAL), (dict(dim=-1), EINVAL), (dict(seqlen=-1), EINVAL), (dict(dtype=3), EUNSUPPORTED),
     (dict(width=0), EUNSUPPORTED), (dict(width=5), EUNSUPPORTED), (dict(activation=2), EINVAL),
-    (dict(dim=1 << 16, seqlen=1 << 15), EUNSUPPORTED), (dict(pool=1), EINVAL), (dict(pool=-3, slots=P), EINVAL),
+    (dict(dim=1 << 16, seqlen=1 << 15), EUNSUPPORTED), (dict(dim=1, seqlen=(1 << 31) - 4095), EUNSUPPORTED),
+    (dict(dim=1, seqlen=(1 << 31) - 1), EUNSUPPORTED), (dict(dim=(1 << 31) - 1, seqlen=1), EUNSUPPORTED), (dict(pool=1), EINVAL), (dict(pool=-3, slots=P), EINVAL),
     (dict(batch=65537, pool=70000, slots=P), EUNSUPPORTED),
     *[(dict([(name, None)]), EINVAL) for name in ("x", "weight", "state", "y")],
     *[(dict([(name, P + 2)]), EINVAL) for name in ("x", "weight", "bias", "state", "slots", "lengths", "y")],
