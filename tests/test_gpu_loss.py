@@ -351,3 +351,35 @@ def test_on_named_streams(lb):
     for r, m in zip(got, more):
         assert torch.equal(r[0], want[0]) and torch.equal(r[1], want[1])
         assert torch.equal(m["dx"], grads["dx"]) and torch.equal(m["dweight"], grads["dweight"])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V,D", [(5, 300, 40), (70, 600, 64), (300, 700, 96)])
+def test_rows_of_the_table_that_are_minus_infinity(lb, dtype, T, V, D):
+    """Words that are masked by their rows (tokens of positive elements): no probability, no gradient, loss and the other rows'
+    gradients as of the table without them."""
+    x, w, y = inputs(T, V, D, TYPES[dtype])
+    x, gone = x.abs() + 0.01, torch.arange(0, V, 7, device="cuda")
+    keep = torch.ones(V, dtype=torch.bool, device="cuda")
+    keep[gone] = False
+    y = torch.nonzero(keep)[:, 0][y % int(keep.sum())]
+    masked = w.clone()
+    masked[gone] = -math.inf
+    loss, lse = lb.lbscan_loss_fwd(x, masked, y)
+    d = weights(T)[0]
+    g = lb.lbscan_loss_bwd(x, masked, y, lse=lse, dloss=d)["dweight"]
+    assert torch.isfinite(loss).all() and torch.isfinite(g).all() and not g[gone].any()
+    number = torch.cumsum(keep, 0) - 1
+    check(lb, x, w[keep].contiguous(), number[y])
+    other = lb.lbscan_loss_fwd(x, w[keep].contiguous(), number[y])
+    # (a sum in another order: the bound of the logits, as in check)
+    size = float((x.double().abs() @ w[keep].double().abs().T).max())
+    limit = 2 * (2 * math.sqrt(D) + 8) * U * size + 16 * U * float(lse.abs().max())
+    assert float((lse - other[1]).abs().max()) <= limit and float((loss - other[0]).abs().max()) <= 2 * limit
+    want = lb.lbscan_loss_bwd(x, w[keep].contiguous(), number[y], lse=other[1], dloss=d)["dweight"]
+    p = torch.softmax(x.double() @ w[keep].double().T, 1) * d[:, None]
+    p[torch.arange(T, device="cuda"), number[y]] += d.double()
+    terms = p.T @ x.double().abs()
+    step = HALF_STEP if x.dtype == torch.bfloat16 else U
+    relative = 2 * limit + 8 * U * (1 + float(lse.abs().max())) + (2 * math.sqrt(T) + 8) * U + (HALF_STEP if x.dtype == torch.bfloat16 else 0)
+    assert bool(((g[keep].double() - want.double()).abs() <= 2 * relative * terms + 2 * step * want.double().abs()).all())
