@@ -185,6 +185,34 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(const T* __restrict__ 
         copy_row<T>(out + r * dimp, there ? x + (long)order[r] * dim : x, there ? dim : 0, dimp, threadIdx.x & 63);
     }
 }
+// At most 64 tokens: all of that in one launch, a wave a row; each of them finds its token from the targets (two launches, one
+// behind the other, were 9 of 30 us of the loss of 64 x 50000 x 768 in bf16).
+template <typename T>
+__global__ __launch_bounds__(256) void loss_few_kernel(const Sources s, const T* __restrict__ x, T* __restrict__ out, const Numbering o, int dim, int dimp)
+{
+    const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int id = lane < s.tokens ? target_of(s, lane) : -1;
+    const unsigned long long there = __ballot(id >= 0);
+    const int live = __popcll(there), mine = __popcll(there & ((1ull << lane) - 1));
+    if (r < 64) {
+        const int token = __ffsll(__ballot(id >= 0 && mine == r)) - 1;
+        copy_row<T>(out + (long)r * dimp, token < 0 ? x : x + (long)token * dim, token < 0 ? 0 : dim, dimp, lane);
+        return;
+    }
+    if (r > 64) return;                        // one wave more
+    if (lane < s.tokens) o.rank[lane] = id >= 0 ? mine : -1;
+    if (lane >= live) o.targets[lane] = -1;
+    if (id >= 0) {
+        o.targets[mine] = id;
+        if (o.lse2) {
+            const float down = o.dloss ? o.dloss[lane] : 0.0f;
+            o.lse2[mine] = o.lse[lane] * kLog2e;
+            o.down[mine] = down;
+            o.both[mine] = down + (o.dlse ? o.dlse[lane] : 0.0f);
+        }
+    }
+    choose(o.choice, o.cuts, live);
+}
 template <typename T>
 __global__ __launch_bounds__(256) void loss_rows_kernel(const T* __restrict__ from, T* __restrict__ to, long rows, int dim, int dimp)
 {
@@ -231,29 +259,38 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2)
     s = s * fast_exp2(m - base) + s2 * fast_exp2(m2 - base);
     m = top;
 }
-// lse and loss of 16 tokens a block, 16 threads to each.
+// lse and loss of TOKENS tokens a block, 256 / TOKENS threads to each.
+template <int TOKENS>
 __global__ __launch_bounds__(256) void loss_join_kernel(const float2* __restrict__ part, const float* __restrict__ own,
                                                         const int* __restrict__ rank, float* __restrict__ loss, float* __restrict__ lse,
                                                         long tokens, int vtiles, const LossChoice* __restrict__ choice)
 {
+    constexpr int kPieces = 256 / TOKENS;
     const long rows = choice->rows, chunks = loss_ceil(vtiles, choice->chunk_lse);
-    __shared__ float2 folds[16][17];
-    const int at = threadIdx.x & 15, piece = threadIdx.x >> 4;
-    for (long first = (long)blockIdx.x * 16; first < tokens; first += (long)gridDim.x * 16) {
+    __shared__ float2 folds[kPieces][TOKENS + 1];
+    const int at = threadIdx.x % TOKENS, piece = threadIdx.x / TOKENS;
+    for (long first = (long)blockIdx.x * TOKENS; first < tokens; first += (long)gridDim.x * TOKENS) {
         const long t = first + at;
         const int r = t < tokens ? rank[t] : -1;
         float m = -INFINITY, s = 0.0f;
         if (r >= 0) {
 #pragma unroll 4
-            for (int c = piece; c < chunks; c += 16) {
+            for (int c = piece; c < chunks; c += kPieces) {
                 const float2 q = part[(long)c * rows + r];
                 join(m, s, q.x, q.y);
             }
         }
         folds[piece][at] = float2{m, s};
         __syncthreads();
+        for (int half = kPieces / 2; half >= 8; half /= 2) {
+            if (piece < half) {
+                join(m, s, folds[piece + half][at].x, folds[piece + half][at].y);
+                folds[piece][at] = float2{m, s};
+            }
+            __syncthreads();
+        }
         if (piece == 0 && t < tokens) {
-            for (int k = 1; k < 16; ++k) join(m, s, folds[k][at].x, folds[k][at].y);
+            for (int k = 1; k < 8; ++k) join(m, s, folds[k][at].x, folds[k][at].y);
             const float v = r >= 0 ? (m + fast_log2(s)) * kLn2 : 0.0f;
             lse[t] = v;
             loss[t] = r >= 0 ? v - own[r] : 0.0f;
@@ -356,7 +393,7 @@ hipError_t pack(const LossParams& p, const LossPlan& plan, const Scratch& s, boo
     const Sources src{p.tokens, p.vocab, p.wide_ids, p.targets};
     const long groups = (p.tokens + kGroup - 1) / kGroup;
     int* counts = s.at<int>(plan.counts);
-    if (groups > 1) {
+    if (groups > 1) {                                          // (the first group needs no counts)
         loss_count_kernel<<<(unsigned)groups, 256, 0, stream>>>(src, counts);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -365,12 +402,19 @@ hipError_t pack(const LossParams& p, const LossPlan& plan, const Scratch& s, boo
                 Cuts{p.vocab, plan.dimp, plan.piece, plan.few, (int)sizeof(T), plan.part_room, plan.acc_rows, plan.share_rows},
                 nullptr, nullptr, nullptr, p.lse, p.dloss, p.dlse};
     if (backward) { o.lse2 = s.at<float>(plan.lse2); o.down = s.at<float>(plan.down); o.both = s.at<float>(plan.both); }
-    loss_rank_kernel<<<(unsigned)groups, 256, 0, stream>>>(src, counts, o);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    loss_gather_kernel<T><<<some(plan.rows / 4), 256, 0, stream>>>(static_cast<const T*>(p.x), s.at<T>(plan.x), o.order, o.targets, o.choice,
-                                                                 plan.rows, p.dim, plan.dimp, loss_tokens(plan.few, sizeof(T)));
-    e = hipGetLastError();
+    const T* x = static_cast<const T*>(p.x);
+    hipError_t e;
+    if (plan.few) {
+        loss_few_kernel<T><<<17, 256, 0, stream>>>(src, x, s.at<T>(plan.x), o, p.dim, plan.dimp);
+        e = hipGetLastError();
+    } else {
+        loss_rank_kernel<<<(unsigned)groups, 256, 0, stream>>>(src, counts, o);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        loss_gather_kernel<T><<<some(plan.rows / 4), 256, 0, stream>>>(x, s.at<T>(plan.x), o.order, o.targets, o.choice, plan.rows, p.dim,
+                                                                     plan.dimp, loss_tokens(0, sizeof(T)));
+        e = hipGetLastError();
+    }
     if (e != hipSuccess || !plan.copy_weight) return e;
     loss_rows_kernel<T><<<some((p.vocab + 3L) / 4), 256, 0, stream>>>(static_cast<const T*>(p.weight), s.at<T>(plan.w), p.vocab, p.dim, plan.dimp);
     return hipGetLastError();
@@ -413,8 +457,11 @@ hipError_t forward(const LossParams& p, const LossPlan& plan, const Scratch& s, 
     t.part = s.at<float2>(plan.part);
     e = (sizeof(T) == 4 ? launch_loss_tiles_f32 : launch_loss_tiles_bf16)(LossKind::lse, t, plan.few, stream);
     if (e != hipSuccess) return e;
-    loss_join_kernel<<<some((p.tokens + 15) / 16), 256, 0, stream>>>(t.part, t.own, s.at<int>(plan.rank), p.loss, p.lse, p.tokens,
-                                                                   (int)loss_ceil(p.vocab, plan.few ? kLossFewVocab : kLossTile), t.choice);
+    const int vtiles = (int)loss_ceil(p.vocab, plan.few ? kLossFewVocab : kLossTile);
+    if (plan.few) loss_join_kernel<4><<<some((p.tokens + 3) / 4), 256, 0, stream>>>(t.part, t.own, s.at<int>(plan.rank), p.loss, p.lse, p.tokens,
+                                                                                  vtiles, t.choice);
+    else loss_join_kernel<16><<<some((p.tokens + 15) / 16), 256, 0, stream>>>(t.part, t.own, s.at<int>(plan.rank), p.loss, p.lse, p.tokens, vtiles,
+                                                                            t.choice);
     return hipGetLastError();
 }
 
