@@ -422,8 +422,8 @@ size_t lbscan_block_norm_workspace_bytes(const lbscan_block_norm_args *args);
  * dweight, and its row of x is not looked at.  Logits, maxima and sums are fp32.  The gradients are
  *     G[t,v] = (dloss[t] + dlse[t]) exp(l[t,v] - lse[t]) - dloss[t] (v == targets[t])
  *     dx[t,:] = scale * sum_v G[t,v] weight[v,:]      dweight[v,:] = scale * sum_t G[t,v] x[t,:]
- * with G made again in pieces of the vocabulary, in the storage type (a factor of the products, as x and weight are), and both
- * sums in fp32. */
+ * with G made again in pieces of the vocabulary, in the storage type (a factor of the products, as x and weight are; what
+ * rounding G[t,targets[t]] to bf16 leaves is added by itself), and both sums in fp32. */
 typedef struct lbscan_loss_args {
     int64_t tokens;               /* <= 2^24; 0: only zeros are written to dweight */
     int32_t vocab, dim;           /* vocab < 2^30; dim in 1 .. 65536 */
