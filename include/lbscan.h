@@ -431,8 +431,8 @@ typedef struct lbscan_loss_args {
     int32_t ids_type;             /* LBSCAN_IDS_* */
     float scale;                  /* finite */
     const void *x;                /* (tokens, dim) */
-    const void *weight;           /* (vocab, dim).  Rows of whole 64 bytes from an address that 16 divides are read in
-                                     place, others are copied to the workspace first */
+    const void *weight;           /* (vocab, dim).  Rows that are no whole 64 bytes, or whose address 16 does not
+                                     divide, are copied to the workspace first where there are more than 64 tokens */
     const void *targets;          /* (tokens) */
     float      *loss;             /* (tokens) out of the forward call */
     float      *lse;              /* (tokens) out of the forward call, read by the backward call */

@@ -35,7 +35,7 @@ hipError_t launch_loss_bwd(const LossParams& p, const LossPlan& plan, void* work
 // The products' launches, one translation unit for each storage type (lbscan_loss_tile.inc).
 struct LossTiles {
     const LossChoice* choice;
-    const void* w;                    // (vocab, ldw), rows of whole steps along dim
+    const void* w;                    // (vocab, ldw), rows of whole steps along dim; loose: of dim, at any element's address
     const void* x;                    // (rows, dimp): the live rows, then zeros to a whole tile
     void* g;                          // (rows, piece)
     const int* targets;               // (rows)
@@ -56,7 +56,7 @@ struct LossTiles {
     float scale;
 };
 enum class LossKind { lse, slope, dx, dweight };
-hipError_t launch_loss_tiles_f32(LossKind kind, const LossTiles& p, int few, hipStream_t stream);
-hipError_t launch_loss_tiles_bf16(LossKind kind, const LossTiles& p, int few, hipStream_t stream);
+hipError_t launch_loss_tiles_f32(LossKind kind, const LossTiles& p, int few, int loose, hipStream_t stream);
+hipError_t launch_loss_tiles_bf16(LossKind kind, const LossTiles& p, int few, int loose, hipStream_t stream);
 
 }  // namespace lbscan

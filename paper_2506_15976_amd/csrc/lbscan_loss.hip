@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256) void loss_count_kernel(const Sources s, int* _
 
 // How the products are cut.
 struct Cuts {
-    int vocab, dimp, piece, few, element;
+    int vocab, dimp, piece, few, loose, element;
     long part_room, acc_rows, share_rows;
 };
 // The lane's candidate of smallest time, found by a wave.
@@ -73,13 +73,13 @@ __device__ int best_chunk(int ntiles, int vtiles, int steps, int units, int most
 __device__ int best_splits(long tiles, int steps, int units, int element, long most)
 {
     const int splits = (threadIdx.x & 63) + 1;
-    const bool fits = splits <= kLossMostSplits && loss_split_fits(steps, splits, most);
+    const bool fits = splits <= loss_most_splits(units) && loss_split_fits(steps, splits, most);
     return best_of(fits ? loss_split_time(tiles, steps, splits, units, element) : INFINITY, splits);
 }
 __device__ void choose(LossChoice* out, const Cuts& c, int live)
 {
     const int ntile = loss_tokens(c.few, c.element), wtile = loss_tokens(0, c.element), vtile = c.few ? kLossFewVocab : kLossTile;
-    const int units = loss_units(c.few), step = 64 / c.element, ntiles = loss_ceil32(live, ntile);
+    const int units = loss_units(c.few, c.loose), step = 64 / c.element, ntiles = loss_ceil32(live, ntile);
     LossChoice r{};
     r.live = live;
     r.rows = ntiles * ntile;
@@ -220,20 +220,32 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(const T* __restrict__ fr
         copy_row<T>(to + r * dimp, from + r * dim, dim, dimp, threadIdx.x & 63);
 }
 
+// E elements of a row of `end` from c, zeros behind it.
+template <int E, typename T>
+__device__ __forceinline__ Pack<T, E> part_of(const T* __restrict__ row, int c, int end)
+{
+    if (c + E <= end) return *reinterpret_cast<const Pack<T, E>*>(row + c);
+    Pack<T, E> q;
+#pragma unroll
+    for (int k = 0; k < E; ++k) q.v[k] = c + k < end ? row[c + k] : T{};
+    return q;
+}
+
 // bf16: the slopes at the targets, rounded for G, and what is left of them; with rest_rows that times the tokens' rows.  A
 // wave a token.
 __global__ __launch_bounds__(256) void loss_target_kernel(const bf16_t* __restrict__ x, const bf16_t* __restrict__ w, const int* __restrict__ targets,
                                                           const float* __restrict__ lse2, const float* __restrict__ down,
                                                           const float* __restrict__ both, float* __restrict__ hot, float* __restrict__ rest,
-                                                          bf16_t* __restrict__ rest_rows, const LossChoice* __restrict__ choice, int dimp, float scale)
+                                                          bf16_t* __restrict__ rest_rows, const LossChoice* __restrict__ choice, int dimp,
+                                                          int ldw, float scale)
 {
     const int live = choice->live, lane = threadIdx.x & 63;
     for (long r = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < live; r += (long)gridDim.x * 4) {
-        const bf16_t *mine = x + r * dimp, *row = w + (long)targets[r] * dimp;
+        const bf16_t *mine = x + r * dimp, *row = w + (long)targets[r] * ldw;
         float dot = 0.0f;
 #pragma unroll 2
         for (int c = lane * 8; c < dimp; c += 512) {
-            const Pack<bf16_t, 8> a = *reinterpret_cast<const Pack<bf16_t, 8>*>(mine + c), b = *reinterpret_cast<const Pack<bf16_t, 8>*>(row + c);
+            const Pack<bf16_t, 8> a = *reinterpret_cast<const Pack<bf16_t, 8>*>(mine + c), b = part_of<8>(row, c, ldw);
 #pragma unroll
             for (int k = 0; k < 8; ++k) dot = fmaf(to_f32(a.v[k]), to_f32(b.v[k]), dot);
         }
@@ -302,7 +314,8 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const float2* __restrict
 // dx: the sums' parts added in their order, in their tokens' places; zeros for the others.  A wave has 256 columns of a token.
 template <typename T>
 __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ acc, const int* __restrict__ rank, const float* __restrict__ rest,
-                                                      const int* __restrict__ targets, const T* __restrict__ weight, T* __restrict__ dx, long tokens, int dim, int dimp, const LossChoice* __restrict__ choice, float scale)
+                                                      const int* __restrict__ targets, const T* __restrict__ weight, T* __restrict__ dx, long tokens, int dim,
+                                                      int dimp, int ldw, const LossChoice* __restrict__ choice, float scale)
 {
     const long rows = choice->rows;
     const int splits = choice->splits_x, strips = (dim + 255) / 256;
@@ -320,7 +333,7 @@ __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ 
                 for (int i = 0; i < 4; ++i) v[i] += q.v[i];
             }
             if constexpr (sizeof(T) == 2) {
-                const Pack<T, 4> row = *reinterpret_cast<const Pack<T, 4>*>(weight + (long)targets[r] * dimp + c);
+                const Pack<T, 4> row = part_of<4>(weight + (long)targets[r] * ldw, c, ldw);
                 const float left = rest[r];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] = fmaf(left, to_f32(row.v[i]), v[i]);
@@ -399,7 +412,7 @@ hipError_t pack(const LossParams& p, const LossPlan& plan, const Scratch& s, boo
         if (e != hipSuccess) return e;
     }
     Numbering o{s.at<int>(plan.rank), s.at<int>(plan.order), s.at<int>(plan.targets), s.at<LossChoice>(plan.choice),
-                Cuts{p.vocab, plan.dimp, plan.piece, plan.few, (int)sizeof(T), plan.part_room, plan.acc_rows, plan.share_rows},
+                Cuts{p.vocab, plan.dimp, plan.piece, plan.few, plan.loose, (int)sizeof(T), plan.part_room, plan.acc_rows, plan.share_rows},
                 nullptr, nullptr, nullptr, p.lse, p.dloss, p.dlse};
     if (backward) { o.lse2 = s.at<float>(plan.lse2); o.down = s.at<float>(plan.down); o.both = s.at<float>(plan.both); }
     const T* x = static_cast<const T*>(p.x);
@@ -428,7 +441,7 @@ LossTiles tiles_of(const LossParams& p, const LossPlan& plan, const Scratch& s)
     t.x = s.at<void>(plan.x);
     t.targets = s.at<int>(plan.targets);
     t.rows = plan.rows;
-    t.vocab = p.vocab; t.dim = p.dim; t.dimp = plan.dimp; t.ldw = plan.dimp; t.piece = plan.piece;
+    t.vocab = p.vocab; t.dim = p.dim; t.dimp = plan.dimp; t.ldw = plan.loose ? p.dim : plan.dimp; t.piece = plan.piece;
     t.first = 0; t.count = p.vocab;
     t.last = 1;
     t.scale = p.scale;
@@ -455,7 +468,7 @@ hipError_t forward(const LossParams& p, const LossPlan& plan, const Scratch& s, 
     LossTiles t = tiles_of(p, plan, s);
     t.own = s.at<float>(plan.own);
     t.part = s.at<float2>(plan.part);
-    e = (sizeof(T) == 4 ? launch_loss_tiles_f32 : launch_loss_tiles_bf16)(LossKind::lse, t, plan.few, stream);
+    e = (sizeof(T) == 4 ? launch_loss_tiles_f32 : launch_loss_tiles_bf16)(LossKind::lse, t, plan.few, plan.loose, stream);
     if (e != hipSuccess) return e;
     const int vtiles = (int)loss_ceil(p.vocab, plan.few ? kLossFewVocab : kLossTile);
     if (plan.few) loss_join_kernel<4><<<some((p.tokens + 3) / 4), 256, 0, stream>>>(t.part, t.own, s.at<int>(plan.rank), p.loss, p.lse, p.tokens,
@@ -481,7 +494,7 @@ hipError_t backward(const LossParams& p, const LossPlan& plan, const Scratch& s,
         bf16_t* rows = p.dweight ? s.at<bf16_t>(plan.rest_rows) : nullptr;
         loss_target_kernel<<<some((p.tokens + 3) / 4), 256, 0, stream>>>(static_cast<const bf16_t*>(t.x), static_cast<const bf16_t*>(t.w), t.targets,
                                                                        t.lse2, t.down, t.both, s.at<float>(plan.hot), s.at<float>(plan.rest), rows,
-                                                                       t.choice, plan.dimp, p.scale);
+                                                                       t.choice, plan.dimp, t.ldw, p.scale);
         e = hipGetLastError();
         if (e == hipSuccess && p.dweight) {
             EmbedParams q = list_params(p, plan);
@@ -499,13 +512,13 @@ hipError_t backward(const LossParams& p, const LossPlan& plan, const Scratch& s,
     for (t.first = 0; t.first < p.vocab && e == hipSuccess; t.first += plan.piece) {
         t.count = p.vocab - t.first < plan.piece ? p.vocab - t.first : plan.piece;
         t.last = t.first + plan.piece >= p.vocab;
-        e = launch(LossKind::slope, t, plan.few, stream);
+        e = launch(LossKind::slope, t, plan.few, plan.loose, stream);
         if (e == hipSuccess && p.dx) {
             t.add = t.first > 0;
-            e = launch(LossKind::dx, t, plan.few, stream);
+            e = launch(LossKind::dx, t, plan.few, plan.loose, stream);
         }
         if (e == hipSuccess && p.dweight) {
-            e = launch(LossKind::dweight, t, plan.few, stream);
+            e = launch(LossKind::dweight, t, plan.few, plan.loose, stream);
             if (e == hipSuccess && plan.share_rows) {
                 loss_dweight_kernel<T><<<some((t.count + 3L) / 4), 256, 0, stream>>>(t.share, static_cast<T*>(p.dweight) + (long)t.first * p.dim, t.count,
                                                                                    p.dim, plan.dimp, t.tokens_of + t.first, t.slot + t.first,
@@ -517,7 +530,7 @@ hipError_t backward(const LossParams& p, const LossPlan& plan, const Scratch& s,
     if (e != hipSuccess || !p.dx) return e;
     loss_dx_kernel<T><<<some((p.tokens * ((p.dim + 255) / 256) + 3) / 4), 256, 0, stream>>>(t.acc, s.at<int>(plan.rank), s.at<float>(plan.rest),
                                                                   t.targets, static_cast<const T*>(t.w), static_cast<T*>(p.dx), p.tokens, p.dim, plan.dimp,
-                                                                  t.choice, p.scale);
+                                                                  t.ldw, t.choice, p.scale);
     return hipGetLastError();
 }
 

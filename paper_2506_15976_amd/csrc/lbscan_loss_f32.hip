@@ -1,8 +1,8 @@
 #include "lbscan_loss_tile.inc"
 
 namespace lbscan {
-hipError_t launch_loss_tiles_f32(LossKind kind, const LossTiles& p, int few, hipStream_t stream)
+hipError_t launch_loss_tiles_f32(LossKind kind, const LossTiles& p, int few, int loose, hipStream_t stream)
 {
-    return launch_typed<float>(kind, p, few, stream);
+    return launch_typed<float>(kind, p, few, loose, stream);
 }
 }  // namespace lbscan

@@ -19,7 +19,9 @@ constexpr int kLossFewTokens = 64, kLossFewVocab = 128;
 // alone keeps the matrix cores as busy: where the last round is not full a compute unit has one.  MI355X, us, logits of
 // 1261 x 32003 x 385: 332 with one block of 256 x 256, 278 with two of 256 x 128; bf16 16384 x 50000 x 768: 1406, 1561.
 LBSCAN_BOTH constexpr int loss_tokens(int few, int element) { return few ? kLossFewTokens : element == 4 ? 128 : 256; }
-constexpr int kLossMostSplits = 32;
+// Parts of a sum.  Loose rows are read by many blocks, or slowly: MI355X, us, dx of 2 x 86816 x 1103 fp32 and 60 x 50000 x 770 bf16 with
+// 32 / 64 parts at most 283 / 191 and 66 / 42 (rows in place, 64 x 50000 x 768: 20 / 22.5).
+LBSCAN_BOTH constexpr int loss_most_splits(int units) { return units == 1024 ? 64 : 32; }
 
 // What the device chooses once the live tokens are counted (the start of the scratch).
 struct LossChoice {
@@ -30,8 +32,8 @@ struct LossChoice {
 
 LBSCAN_BOTH inline long loss_ceil(long a, long b) { return (a + b - 1) / b; }
 LBSCAN_BOTH inline int loss_ceil32(int a, int b) { return (a + b - 1) / b; }
-// Compute units, whose rounds of units of the products are counted; of few tokens three blocks run on one at once.
-LBSCAN_BOTH constexpr int loss_units(int few) { return few ? 768 : 256; }
+// Compute units, whose rounds of units of the products are counted; of few tokens three blocks run on one at once, four with loose rows.
+LBSCAN_BOTH constexpr int loss_units(int few, int loose) { return loose ? 1024 : few ? 768 : 256; }
 
 // Time of the logits' products in steps, in units of `chunk` of `vtiles` tiles of the vocabulary for each of `ntiles` tiles of
 // tokens: whole rounds of the machine.  A tile's exponentials take about as long as 6 steps, a unit's first loads 3.
@@ -46,14 +48,15 @@ LBSCAN_BOTH inline int loss_chunk_of(int ntiles, int vtiles, int rounds, int uni
     return loss_ceil32(vtiles, chunks < 1 ? 1 : chunks > vtiles ? vtiles : chunks);
 }
 // Time of a sum over `steps` steps for `tiles` tiles, cut into `splits` parts, which are written and read once more (4 bytes a
-// value at about 4.5 TB/s: 0.12 us a tile of 256 x 256, of 1.0 us a step in bf16, 0.06 us one of 256 x 128, of 1.8 us in fp32).
+// value at about 4.5 TB/s: 0.12 us a tile of 256 x 256, of 1.0 us a step in bf16, 0.06 us one of 256 x 128, of 1.8 us in fp32; steps of
+// loose rows are those of memory, 0.4 us, of 0.015 us a tile).
 LBSCAN_BOTH inline float loss_split_time(long tiles, int steps, int splits, int units, int element)
 {
     const float all = (float)tiles * (float)splits;
     float rounds = ceilf(all / (float)units);
     // (fp32: a block alone on its compute unit takes about a quarter longer than half the time of two)
-    if (element == 4 && ceilf(rounds / 2.0f) * 2.0f != rounds) rounds += 0.25f;
-    return rounds * (float)(loss_ceil32(steps, splits) + 4) + (splits > 1 ? (element == 2 ? 0.12f : 0.035f) * all : 0.0f);
+    if (element == 4 && units < 1024 && ceilf(rounds / 2.0f) * 2.0f != rounds) rounds += 0.25f;
+    return rounds * (float)(loss_ceil32(steps, splits) + 4) + (splits > 1 ? (element == 2 && units < 1024 ? 0.12f : 0.035f) * all : 0.0f);
 }
 LBSCAN_BOTH inline bool loss_split_fits(int steps, int splits, long most) { return splits == 1 || (splits <= most && splits * 8 <= steps); }
 
@@ -61,7 +64,8 @@ struct LossPlan {
     int dimp;                // dim in whole steps of the products (64 bytes)
     long rows;               // tokens in whole tiles
     int few;                 // tiles of 64 tokens
-    int copy_weight;         // the table's rows are no whole steps, or not aligned
+    int loose;               // the table's rows are no whole steps, or not aligned: few tokens read them as they are,
+    int copy_weight;         // others a copy
     int piece, pieces;       // columns of the vocabulary that G has room for
     long part_room;          // values of the forward pass's parts (rows x chunks)
     long acc_rows;           // rows of dx's sums (rows x splits)
@@ -74,8 +78,8 @@ struct LossPlan {
 inline int loss_best_splits(long tiles, int steps, int units, int element)
 {
     int best = 1;
-    for (int s = 2; s <= kLossMostSplits; ++s)
-        if (loss_split_fits(steps, s, kLossMostSplits) &&
+    for (int s = 2; s <= loss_most_splits(units); ++s)
+        if (loss_split_fits(steps, s, loss_most_splits(units)) &&
             loss_split_time(tiles, steps, s, units, element) < loss_split_time(tiles, steps, best, units, element))
             best = s;
     return best;
@@ -89,9 +93,11 @@ inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool 
     const int step = 64 / element;
     p.dimp = (int)(loss_ceil(dim, step) * step);
     p.few = tokens <= kLossFewTokens;
-    const int ntile = loss_tokens(p.few, element), wtile = loss_tokens(0, element), units = loss_units(p.few);
+    const bool whole_rows = dim == p.dimp && aligned;
+    p.loose = p.few && !whole_rows;
+    p.copy_weight = !p.few && !whole_rows;
+    const int ntile = loss_tokens(p.few, element), wtile = loss_tokens(0, element), units = loss_units(p.few, p.loose);
     p.rows = loss_ceil(tokens, ntile) * ntile;
-    p.copy_weight = dim != p.dimp || !aligned;
     const long mtiles = loss_ceil(p.dimp, kLossTile), vtiles = loss_ceil(vocab, kLossTile);
     // G: at most a gigabyte of the vocabulary at a time, in pieces that are just a whole number of rounds of dweight's tiles
     long most = ((long)1 << 30) / (p.rows * element) / kLossTile;

@@ -8,7 +8,7 @@ import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2506_15976_amd", "csrc")
-NUMBERS = ("dimp", "rows", "few", "copy_weight", "piece", "pieces", "part_room", "acc_rows", "share_rows")
+NUMBERS = ("dimp", "rows", "few", "loose", "copy_weight", "piece", "pieces", "part_room", "acc_rows", "share_rows")
 FIELDS = ("choice", "counts", "rank", "order", "targets", "lse2", "down", "both", "own", "part", "x", "w", "g", "acc", "share", "hot", "rest",
           "rest_rows", "list", "slot", "sort", "total")
 
@@ -48,7 +48,8 @@ def test_sizes_and_scratch(plan):
         tile = 64 if p["few"] else 256 if e == 2 else 128
         assert p["dimp"] % (64 // e) == 0 and 0 <= p["dimp"] - D < 64 // e
         assert p["rows"] % tile == 0 and 0 <= p["rows"] - T < tile
-        assert p["copy_weight"] == int(not aligned or D % (64 // e) != 0)
+        odd = not aligned or D % (64 // e) != 0
+        assert p["copy_weight"] == int(odd and not p["few"]) and p["loose"] == int(odd and p["few"])
         # the pieces cover the vocabulary, none is empty, and the offsets of a block's lines fit 32 bits
         assert p["piece"] % 256 == 0 and (p["pieces"] - 1) * p["piece"] < V <= p["pieces"] * p["piece"]
         assert p["piece"] * e * 256 < 1 << 32 and p["dimp"] * e * 256 < 1 << 32
