@@ -383,3 +383,17 @@ def test_rows_of_the_table_that_are_minus_infinity(lb, dtype, T, V, D):
     step = HALF_STEP if x.dtype == torch.bfloat16 else U
     relative = 2 * limit + 8 * U * (1 + float(lse.abs().max())) + (2 * math.sqrt(T) + 8) * U + (HALF_STEP if x.dtype == torch.bfloat16 else 0)
     assert bool(((g[keep].double() - want.double()).abs() <= 2 * relative * terms + 2 * step * want.double().abs()).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("before", [1, 8, 64])
+@pytest.mark.parametrize("T,V,D", [(1, 129, 64), (7, 300, 65), (40, 257, 33), (64, 700, 100), (64, 1100, 257), (65, 300, 100), (33, 130, 1)])
+def test_tables_between_no_numbers(lb, dtype, before, T, V, D):
+    """Rows of any length and address, read where they are or copied: what stands in front of and behind them is not used."""
+    def between(t):
+        flat = torch.full((t.numel() + before + 64,), math.nan, device="cuda", dtype=t.dtype)
+        inner = flat[before:before + t.numel()].view(t.shape)
+        inner.copy_(t)
+        return inner
+    x, w, y = inputs(T, V, D, TYPES[dtype], ignored=0.1)
+    check(lb, between(x), between(w), y, dloss=weights(T)[0], dlse=weights(T)[1])
