@@ -14,6 +14,7 @@
 namespace lbscan {
 
 constexpr int kLossTile = 256;                // rows of the table, or columns of x, of a block's product
+constexpr int kLossLooseSteps = 4;            // steps under way of a product with loose rows, which has whole fours of them
 constexpr int kLossFewTokens = 64, kLossFewVocab = 128;
 // Tokens (of dweight: rows of the table) of a block's product.  fp32: half as many and two blocks a compute unit, of which one
 // alone keeps the matrix cores as busy: where the last round is not full a compute unit has one.  MI355X, us, logits of
@@ -21,7 +22,7 @@ constexpr int kLossFewTokens = 64, kLossFewVocab = 128;
 LBSCAN_BOTH constexpr int loss_tokens(int few, int element) { return few ? kLossFewTokens : element == 4 ? 128 : 256; }
 // Parts of a sum.  Loose rows are read by many blocks, or slowly: MI355X, us, dx of 2 x 86816 x 1103 fp32 and 60 x 50000 x 770 bf16 with
 // 32 / 64 parts at most 283 / 191 and 66 / 42 (rows in place, 64 x 50000 x 768: 20 / 22.5).
-LBSCAN_BOTH constexpr int loss_most_splits(int units) { return units == 1024 ? 64 : 32; }
+LBSCAN_BOTH constexpr int loss_most_splits(int units) { return units == 512 ? 64 : 32; }
 
 // What the device chooses once the live tokens are counted (the start of the scratch).
 struct LossChoice {
@@ -32,8 +33,8 @@ struct LossChoice {
 
 LBSCAN_BOTH inline long loss_ceil(long a, long b) { return (a + b - 1) / b; }
 LBSCAN_BOTH inline int loss_ceil32(int a, int b) { return (a + b - 1) / b; }
-// Compute units, whose rounds of units of the products are counted; of few tokens three blocks run on one at once, four with loose rows.
-LBSCAN_BOTH constexpr int loss_units(int few, int loose) { return loose ? 1024 : few ? 768 : 256; }
+// Compute units, whose rounds of units of the products are counted; of few tokens three blocks run on one at once, two with loose rows.
+LBSCAN_BOTH constexpr int loss_units(int few, int loose) { return loose ? 512 : few ? 768 : 256; }
 
 // Time of the logits' products in steps, in units of `chunk` of `vtiles` tiles of the vocabulary for each of `ntiles` tiles of
 // tokens: whole rounds of the machine.  A tile's exponentials take about as long as 6 steps, a unit's first loads 3.
@@ -55,13 +56,13 @@ LBSCAN_BOTH inline float loss_split_time(long tiles, int steps, int splits, int 
     const float all = (float)tiles * (float)splits;
     float rounds = ceilf(all / (float)units);
     // (fp32: a block alone on its compute unit takes about a quarter longer than half the time of two)
-    if (element == 4 && units < 1024 && ceilf(rounds / 2.0f) * 2.0f != rounds) rounds += 0.25f;
-    return rounds * (float)(loss_ceil32(steps, splits) + 4) + (splits > 1 ? (element == 2 && units < 1024 ? 0.12f : 0.035f) * all : 0.0f);
+    if (element == 4 && units != 512 && ceilf(rounds / 2.0f) * 2.0f != rounds) rounds += 0.25f;
+    return rounds * (float)(loss_ceil32(steps, splits) + 4) + (splits > 1 ? (element == 2 && units != 512 ? 0.12f : 0.035f) * all : 0.0f);
 }
 LBSCAN_BOTH inline bool loss_split_fits(int steps, int splits, long most) { return splits == 1 || (splits <= most && splits * 8 <= steps); }
 
 struct LossPlan {
-    int dimp;                // dim in whole steps of the products (64 bytes)
+    int dimp;                // dim in whole steps of the products (64 bytes), loose: in fours of them
     long rows;               // tokens in whole tiles
     int few;                 // tiles of 64 tokens
     int loose;               // the table's rows are no whole steps, or not aligned: few tokens read them as they are,
@@ -91,11 +92,12 @@ inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool 
     LossPlan p{};
     if (tokens == 0 || vocab == 0 || dim == 0) return p;        // (no kernel runs)
     const int step = 64 / element;
-    p.dimp = (int)(loss_ceil(dim, step) * step);
     p.few = tokens <= kLossFewTokens;
-    const bool whole_rows = dim == p.dimp && aligned;
-    p.loose = p.few && !whole_rows;
-    p.copy_weight = !p.few && !whole_rows;
+    const bool whole_rows = dim % step == 0 && aligned;
+    p.loose = p.few && !whole_rows && dim * element >= 16;
+    p.copy_weight = !whole_rows && !p.loose;
+    const int whole = p.loose ? step * kLossLooseSteps : step;
+    p.dimp = (int)(loss_ceil(dim, whole) * whole);
     const int ntile = loss_tokens(p.few, element), wtile = loss_tokens(0, element), units = loss_units(p.few, p.loose);
     p.rows = loss_ceil(tokens, ntile) * ntile;
     const long mtiles = loss_ceil(p.dimp, kLossTile), vtiles = loss_ceil(vocab, kLossTile);

@@ -46,10 +46,11 @@ def test_sizes_and_scratch(plan):
         aligned, backward, dx, dw = (rng.randrange(2) for _ in range(4))
         p = plan(T, V, D, e, aligned, backward, dx, dw)
         tile = 64 if p["few"] else 256 if e == 2 else 128
-        assert p["dimp"] % (64 // e) == 0 and 0 <= p["dimp"] - D < 64 // e
+        whole = 256 // e if p["loose"] else 64 // e
+        assert p["dimp"] % whole == 0 and 0 <= p["dimp"] - D < whole
         assert p["rows"] % tile == 0 and 0 <= p["rows"] - T < tile
         odd = not aligned or D % (64 // e) != 0
-        assert p["copy_weight"] == int(odd and not p["few"]) and p["loose"] == int(odd and p["few"])
+        assert p["loose"] == int(odd and p["few"] and D * e >= 16) and p["copy_weight"] == int(odd and not p["loose"])
         # the pieces cover the vocabulary, none is empty, and the offsets of a block's lines fit 32 bits
         assert p["piece"] % 256 == 0 and (p["pieces"] - 1) * p["piece"] < V <= p["pieces"] * p["piece"]
         assert p["piece"] * e * 256 < 1 << 32 and p["dimp"] * e * 256 < 1 << 32
