@@ -432,7 +432,8 @@ typedef struct lbscan_loss_args {
     float scale;                  /* finite */
     const void *x;                /* (tokens, dim) */
     const void *weight;           /* (vocab, dim).  Rows that are no whole 64 bytes, or whose address 16 does not
-                                     divide, are copied to the workspace first where there are more than 64 tokens */
+                                     divide, are copied to the workspace first where there are more than 64
+                                     tokens (or a row has less than 16 bytes) */
     const void *targets;          /* (tokens) */
     float      *loss;             /* (tokens) out of the forward call */
     float      *lse;              /* (tokens) out of the forward call, read by the backward call */

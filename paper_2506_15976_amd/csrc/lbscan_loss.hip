@@ -78,8 +78,8 @@ __device__ int best_splits(long tiles, int steps, int units, int element, long m
 }
 __device__ void choose(LossChoice* out, const Cuts& c, int live)
 {
-    const int ntile = loss_tokens(c.few, c.element), wtile = loss_tokens(0, c.element), vtile = c.few ? kLossFewVocab : kLossTile;
-    const int units = loss_units(c.few, c.loose), step = 64 / c.element, ntiles = loss_ceil32(live, ntile);
+    const int ntile = loss_tokens(c.few, c.element), wtile = loss_tokens(0, c.element), vtile = c.few ? loss_few_vocab(c.loose, c.element) : kLossTile;
+    const int units = loss_units(c.few, c.loose, c.element), step = 64 / c.element, ntiles = loss_ceil32(live, ntile);
     LossChoice r{};
     r.live = live;
     r.rows = ntiles * ntile;
@@ -470,7 +470,7 @@ hipError_t forward(const LossParams& p, const LossPlan& plan, const Scratch& s, 
     t.part = s.at<float2>(plan.part);
     e = (sizeof(T) == 4 ? launch_loss_tiles_f32 : launch_loss_tiles_bf16)(LossKind::lse, t, plan.few, plan.loose, stream);
     if (e != hipSuccess) return e;
-    const int vtiles = (int)loss_ceil(p.vocab, plan.few ? kLossFewVocab : kLossTile);
+    const int vtiles = (int)loss_ceil(p.vocab, plan.few ? loss_few_vocab(plan.loose, sizeof(T)) : kLossTile);
     if (plan.few) loss_join_kernel<4><<<some((p.tokens + 3) / 4), 256, 0, stream>>>(t.part, t.own, s.at<int>(plan.rank), p.loss, p.lse, p.tokens,
                                                                                   vtiles, t.choice);
     else loss_join_kernel<16><<<some((p.tokens + 15) / 16), 256, 0, stream>>>(t.part, t.own, s.at<int>(plan.rank), p.loss, p.lse, p.tokens, vtiles,

@@ -15,14 +15,18 @@ namespace lbscan {
 
 constexpr int kLossTile = 256;                // rows of the table, or columns of x, of a block's product
 constexpr int kLossLooseSteps = 4;            // steps under way of a product with loose rows, which has whole fours of them
-constexpr int kLossFewTokens = 64, kLossFewVocab = 128;
+constexpr int kLossFewTokens = 64;
+// Rows of the table (columns of x) of few tokens' products.  fp32 with loose rows: half as many, as a compute unit with one block is bound by
+// its matrix cores (MI355X, us, loss and gradients, 128 / 64: 35 x 11565 x 2753 fp32 377 / 279; 3 x 129028 x 2610 bf16 866 / 967).
+LBSCAN_BOTH constexpr int loss_few_vocab(int loose, int element) { return loose && element == 4 ? 64 : 128; }
 // Tokens (of dweight: rows of the table) of a block's product.  fp32: half as many and two blocks a compute unit, of which one
 // alone keeps the matrix cores as busy: where the last round is not full a compute unit has one.  MI355X, us, logits of
 // 1261 x 32003 x 385: 332 with one block of 256 x 256, 278 with two of 256 x 128; bf16 16384 x 50000 x 768: 1406, 1561.
 LBSCAN_BOTH constexpr int loss_tokens(int few, int element) { return few ? kLossFewTokens : element == 4 ? 128 : 256; }
 // Parts of a sum.  Loose rows are read by many blocks, or slowly: MI355X, us, dx of 2 x 86816 x 1103 fp32 and 60 x 50000 x 770 bf16 with
 // 32 / 64 parts at most 283 / 191 and 66 / 42 (rows in place, 64 x 50000 x 768: 20 / 22.5).
-LBSCAN_BOTH constexpr int loss_most_splits(int units) { return units == 512 ? 64 : 32; }
+LBSCAN_BOTH constexpr bool loss_loose_units(int units) { return units == 512 || units == 1024; }
+LBSCAN_BOTH constexpr int loss_most_splits(int units) { return loss_loose_units(units) ? 64 : 32; }
 
 // What the device chooses once the live tokens are counted (the start of the scratch).
 struct LossChoice {
@@ -33,8 +37,8 @@ struct LossChoice {
 
 LBSCAN_BOTH inline long loss_ceil(long a, long b) { return (a + b - 1) / b; }
 LBSCAN_BOTH inline int loss_ceil32(int a, int b) { return (a + b - 1) / b; }
-// Compute units, whose rounds of units of the products are counted; of few tokens three blocks run on one at once, two with loose rows.
-LBSCAN_BOTH constexpr int loss_units(int few, int loose) { return loose ? 512 : few ? 768 : 256; }
+// Compute units, whose rounds of units of the products are counted; of few tokens three blocks run on one at once, with loose rows two, in fp32 four.
+LBSCAN_BOTH constexpr int loss_units(int few, int loose, int element) { return loose ? (element == 4 ? 1024 : 512) : few ? 768 : 256; }
 
 // Time of the logits' products in steps, in units of `chunk` of `vtiles` tiles of the vocabulary for each of `ntiles` tiles of
 // tokens: whole rounds of the machine.  A tile's exponentials take about as long as 6 steps, a unit's first loads 3.
@@ -56,8 +60,8 @@ LBSCAN_BOTH inline float loss_split_time(long tiles, int steps, int splits, int 
     const float all = (float)tiles * (float)splits;
     float rounds = ceilf(all / (float)units);
     // (fp32: a block alone on its compute unit takes about a quarter longer than half the time of two)
-    if (element == 4 && units != 512 && ceilf(rounds / 2.0f) * 2.0f != rounds) rounds += 0.25f;
-    return rounds * (float)(loss_ceil32(steps, splits) + 4) + (splits > 1 ? (element == 2 && units != 512 ? 0.12f : 0.035f) * all : 0.0f);
+    if (element == 4 && !loss_loose_units(units) && ceilf(rounds / 2.0f) * 2.0f != rounds) rounds += 0.25f;
+    return rounds * (float)(loss_ceil32(steps, splits) + 4) + (splits > 1 ? (element == 2 && !loss_loose_units(units) ? 0.12f : 0.035f) * all : 0.0f);
 }
 LBSCAN_BOTH inline bool loss_split_fits(int steps, int splits, long most) { return splits == 1 || (splits <= most && splits * 8 <= steps); }
 
@@ -98,7 +102,7 @@ inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool 
     p.copy_weight = !whole_rows && !p.loose;
     const int whole = p.loose ? step * kLossLooseSteps : step;
     p.dimp = (int)(loss_ceil(dim, whole) * whole);
-    const int ntile = loss_tokens(p.few, element), wtile = loss_tokens(0, element), units = loss_units(p.few, p.loose);
+    const int ntile = loss_tokens(p.few, element), wtile = loss_tokens(0, element), units = loss_units(p.few, p.loose, element);
     p.rows = loss_ceil(tokens, ntile) * ntile;
     const long mtiles = loss_ceil(p.dimp, kLossTile), vtiles = loss_ceil(vocab, kLossTile);
     // G: at most a gigabyte of the vocabulary at a time, in pieces that are just a whole number of rounds of dweight's tiles
@@ -122,7 +126,7 @@ inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool 
     if (p.copy_weight) p.w = take((size_t)vocab * p.dimp * element);
     if (!backward) {
         // chunks for up to 64 rounds of units
-        const long all = p.rows * loss_ceil(vocab, p.few ? kLossFewVocab : kLossTile), room = 64L * units * ntile;
+        const long all = p.rows * loss_ceil(vocab, p.few ? loss_few_vocab(p.loose, element) : kLossTile), room = 64L * units * ntile;
         p.part_room = all < room ? all : room < p.rows ? p.rows : room;
         p.own = take(4 * (size_t)p.rows);
         p.part = take(8 * (size_t)p.part_room);
@@ -144,7 +148,7 @@ inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool 
         if (want_dx) {
             // as many parts as all tokens need, and more for fewer live ones
             const long few_rows = p.few ? 1024 : 8192;
-            p.acc_rows = p.rows * loss_best_splits(loss_ceil(p.dimp, p.few ? kLossFewVocab : kLossTile) * (p.rows / ntile), (int)loss_ceil(p.piece, step), units, element);
+            p.acc_rows = p.rows * loss_best_splits(loss_ceil(p.dimp, p.few ? loss_few_vocab(p.loose, element) : kLossTile) * (p.rows / ntile), (int)loss_ceil(p.piece, step), units, element);
             if (p.acc_rows < few_rows) p.acc_rows = few_rows;
             p.acc = take(4 * (size_t)p.acc_rows * p.dimp);
         }
