@@ -397,3 +397,29 @@ def test_tables_between_no_numbers(lb, dtype, before, T, V, D):
         return inner
     x, w, y = inputs(T, V, D, TYPES[dtype], ignored=0.1)
     check(lb, between(x), between(w), y, dloss=weights(T)[0], dlse=weights(T)[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,D", [(40, 64), (40, 65), (64, 130), (1, 33)])
+def test_few_tokens_replayed_in_a_graph(lb, dtype, T, D):
+    x, w, y = inputs(T, 500, D, TYPES[dtype])
+    d, e = weights(T)
+
+    def both():
+        loss, lse = lb.lbscan_loss_fwd(x, w, y)
+        return [loss, lse, *lb.lbscan_loss_bwd(x, w, y, lse=lse, dloss=d, dlse=e).values()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both()
+    for k in range(4):
+        x.normal_()
+        y.copy_(torch.where(torch.rand(T, device="cuda") < 0.3 * k, 500, torch.randint(0, 500, (T,), device="cuda")))
+        graph.replay()
+        want = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
