@@ -27,17 +27,31 @@ __device__ __forceinline__ bool taken(const int32_t* __restrict__ slots, int b, 
 __device__ __forceinline__ float silu_f32(float v) { return v * sigmoid_f32(v); }
 
 // ---- one token -------------------------------------------------------------------------------------------
-// A channel's states are four to a lane, Q lanes to a channel; a block has one row of the batch and 256 / Q channels, U times, so
-// that it reads and writes whole kilobytes of the pool.  Everything is loaded before the search for an earlier row with the same
-// slot ends: only what is stored waits for it.  Bound by memory, read and written in the same places: MI355X, us, 256 rows of
-// 4096 x 16 in bf16 with the convolution, states in a pool (155.6 MB), U = 1 / 2 / 3: 43.9 / 43.4 / 45.2 (3.6 TB/s);
-// with two rows of the batch to a block, whose constants stay in registers, 48.9.  64 rows of 768: 4.1, of which the call is 3.8.
-template <typename T, int Q, int U, int K>
+// A channel's states are four to a lane, Q lanes to a channel.  WIDE: a wave has 64 channels of one row of the batch, and a lane two
+// parts: what a channel has one of (x through the convolution, dt, the gate, y) for channel `lane`, and states of Q channels,
+// to which dt and dt x come from the channels' lanes and from which the sums go back.  Otherwise a wave has U times 64 / Q channels,
+// whose lanes all compute what a channel has one of.  Everything is loaded before the search for an earlier row with the same slot
+// ends: only what is stored waits for it.  Loads of the optional inputs stand in branches, where a sum or a conversion would wait for
+// all loads before it: those come later (256 x 4096 without the convolution 34.2 -> 25.3 us).  Bound by memory, read and written in
+// the same places: MI355X, 256 x 4096 x 16 bf16 with the convolution, states in a pool (155.6 MB) 39.4 us (3.9 TB/s), without it 25.7
+// (5.5 TB/s; a sum in place of that size 26.0).
+template <typename T, int Q, int K, int U, bool WIDE>
 __global__ __launch_bounds__(256) void step_kernel(const StepParams p)
 {
-    constexpr int kChannels = 256 / Q;
-    const int q = threadIdx.x & (Q - 1), N = p.dstate, n0 = 4 * q;
+    constexpr int kGroup = 64 / Q, S = WIDE ? 1 : U;              // channels whose states are updated at once; channels of a lane
+    static_assert(!WIDE || U == Q, "a channel a lane");
+    const int lane = threadIdx.x & 63, N = p.dstate, n0 = 4 * (lane % Q);
+    const int first = (int)(blockIdx.x * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * (kGroup * U);
+    if (first >= p.dim) return;
     const bool whole = n0 + 4 <= N;
+    int d[S];
+    bool channel[S], writer[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        d[s] = first + (WIDE ? lane : s * kGroup + lane / Q);
+        channel[s] = d[s] < p.dim;
+        writer[s] = channel[s] && (WIDE || lane % Q == 0);
+    }
     auto four = [&](const auto* from, float to[4]) {           // the lane's four of N, zeros behind them
         using V = std::remove_cv_t<std::remove_reference_t<decltype(*from)>>;
         if (whole) {
@@ -50,110 +64,144 @@ __global__ __launch_bounds__(256) void step_kernel(const StepParams p)
         }
     };
     for (int b = blockIdx.y; b < p.batch; b += gridDim.y) {
+        T* y = static_cast<T*>(p.y) + (long)b * p.dim;
+        auto padding = [&] {
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                if (writer[s]) y[d[s]] = from_f32<T>(0.0f);
+        };
         const int slot = p.slots ? p.slots[b] : b;
-        const bool inside = (unsigned)slot < (unsigned)p.pool;
-        float h[U][4], a[U][4], bm[4], cm[4], delta[U], z[U], pre[U];
-        Pack<float, (K > 0 ? K : 1)> w[U];
-        Pack<T, (K > 1 ? K - 1 : 1)> old[U];
-        T raw[U];
-        int d[U];
-        bool there[U];
+        if ((unsigned)slot >= (unsigned)p.pool) {
+            padding();
+            continue;
+        }
+        const long row = (long)slot * p.dim;                      // of the pools
+        float h[U][4], a[U][4], bm[4], cm[4];
         four(static_cast<const T*>(p.Bm) + b * p.b_stride + n0, bm);
         four(static_cast<const T*>(p.Cm) + b * p.c_stride + n0, cm);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            d[u] = (blockIdx.x * U + u) * kChannels + threadIdx.x / Q;
-            there[u] = inside && d[u] < p.dim;
-            if (!there[u]) continue;
-            const long at = (long)slot * p.dim + d[u];
-            four(p.state + at * N + n0, h[u]);
-            four(p.A + (long)d[u] * N + n0, a[u]);
-            raw[u] = static_cast<const T*>(p.x)[b * p.x_stride + d[u]];
-            delta[u] = to_f32(static_cast<const T*>(p.delta)[b * p.delta_stride + d[u]]);
-            z[u] = p.z ? to_f32(static_cast<const T*>(p.z)[b * p.z_stride + d[u]]) : 0.0f;
-            if constexpr (K > 0) {
-                pre[u] = p.conv_bias ? p.conv_bias[d[u]] : 0.0f;
-                w[u] = *reinterpret_cast<const Pack<float, K>*>(p.conv_weight + (long)d[u] * K);
-            }
-            if constexpr (K > 1) old[u] = *reinterpret_cast<const Pack<T, K - 1>*>(static_cast<const T*>(p.conv_state) + at * (K - 1));
+            const int of = first + u * kGroup + lane / Q;
+            if (of >= p.dim) continue;
+            four(p.state + (row + of) * N + n0, h[u]);
+            four(p.A + (long)of * N + n0, a[u]);
         }
-        const bool mine = !p.slots || !taken(p.slots, b, slot);
+        float x[S], dt[S], skip[S], bias[S], pre[S], in[S], total[S];
+        Pack<float, (K > 0 ? K : 1)> w[S];
+        Pack<T, (K > 1 ? K - 1 : 1)> old[S];
+        T raw[S], delta[S], gate[S];                              // (converted later: here that would wait for the loads)
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (d[u] >= p.dim) continue;
-            T* y = static_cast<T*>(p.y) + (long)b * p.dim + d[u];
-            if (!there[u] || !mine) {
-                if (q == 0) *y = from_f32<T>(0.0f);
-                continue;
+        for (int s = 0; s < S; ++s) {
+            skip[s] = bias[s] = pre[s] = total[s] = 0.0f;
+            raw[s] = delta[s] = gate[s] = T{};
+            w[s] = {};
+            old[s] = {};
+            if (!channel[s]) continue;
+            raw[s] = static_cast<const T*>(p.x)[b * p.x_stride + d[s]];
+            delta[s] = static_cast<const T*>(p.delta)[b * p.delta_stride + d[s]];
+            if (p.delta_bias) bias[s] = p.delta_bias[d[s]];
+            if (p.z) gate[s] = static_cast<const T*>(p.z)[b * p.z_stride + d[s]];
+            if (p.Dskip) skip[s] = p.Dskip[d[s]];
+            if constexpr (K > 0) {
+                if (p.conv_bias) pre[s] = p.conv_bias[d[s]];
+                w[s] = *reinterpret_cast<const Pack<float, K>*>(p.conv_weight + (long)d[s] * K);
             }
-            const long at = (long)slot * p.dim + d[u];
-            float x = to_f32(raw[u]);
+            if constexpr (K > 1)
+                old[s] = *reinterpret_cast<const Pack<T, K - 1>*>(static_cast<const T*>(p.conv_state) + (row + d[s]) * (K - 1));
+        }
+        if (p.slots && taken(p.slots, b, slot)) {
+            padding();
+            continue;
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            x[s] = to_f32(raw[s]);
             if constexpr (K > 0) {
                 if constexpr (K > 1) {
+                    Pack<T, K - 1> next;
 #pragma unroll
-                    for (int k = 0; k < K - 1; ++k) pre[u] = fmaf(w[u].v[k], to_f32(old[u].v[k]), pre[u]);
-                    if (q == 0) {
-                        Pack<T, K - 1> next;
-#pragma unroll
-                        for (int k = 0; k < K - 1; ++k) next.v[k] = k < K - 2 ? old[u].v[k < K - 2 ? k + 1 : k] : raw[u];
-                        *reinterpret_cast<Pack<T, K - 1>*>(static_cast<T*>(p.conv_state) + at * (K - 1)) = next;
+                    for (int k = 0; k < K - 1; ++k) {
+                        pre[s] = fmaf(w[s].v[k], to_f32(old[s].v[k]), pre[s]);
+                        next.v[k] = k < K - 2 ? old[s].v[k < K - 2 ? k + 1 : k] : raw[s];
                     }
+                    if (writer[s]) *reinterpret_cast<Pack<T, K - 1>*>(static_cast<T*>(p.conv_state) + (row + d[s]) * (K - 1)) = next;
                 }
-                pre[u] = fmaf(w[u].v[K - 1], x, pre[u]);
-                x = p.activation ? silu_f32(pre[u]) : pre[u];
+                pre[s] = fmaf(w[s].v[K - 1], x[s], pre[s]);
+                x[s] = p.activation ? silu_f32(pre[s]) : pre[s];
             }
-            float dt = delta[u] + (p.delta_bias ? p.delta_bias[d[u]] : 0.0f);
-            if (p.softplus) dt = softplus_f32(dt);
-            const float in = dt * x;
+            dt[s] = to_f32(delta[s]) + bias[s];
+            if (p.softplus) dt[s] = softplus_f32(dt[s]);
+            in[s] = dt[s] * x[s];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int from = u * kGroup + lane / Q, of = first + from;
+            const float dtu = WIDE ? __shfl(dt[0], from, 64) : dt[WIDE ? 0 : u], inu = WIDE ? __shfl(in[0], from, 64) : in[WIDE ? 0 : u];
             float sum = 0.0f;
+            if (of < p.dim) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                h[u][i] = fmaf(fast_exp2(dt * a[u][i] * kLog2e), h[u][i], in * bm[i]);
-                // (a lane's places behind N add nothing, also where the input is not finite)
-                sum = n0 + i < N ? fmaf(cm[i], h[u][i], sum) : sum;
-            }
-            float* state = p.state + at * N + n0;
-            if (whole) {
-                Pack<float, 4> v;
+                for (int i = 0; i < 4; ++i) {
+                    h[u][i] = fmaf(fast_exp2(dtu * a[u][i] * kLog2e), h[u][i], inu * bm[i]);
+                    // (a lane's places behind N add nothing, also where the input is not finite)
+                    sum = n0 + i < N ? fmaf(cm[i], h[u][i], sum) : sum;
+                }
+                float* state = p.state + (row + of) * N + n0;
+                if (whole) {
+                    Pack<float, 4> v;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v.v[i] = h[u][i];
-                *reinterpret_cast<Pack<float, 4>*>(state) = v;
-            } else {
+                    for (int i = 0; i < 4; ++i) v.v[i] = h[u][i];
+                    *reinterpret_cast<Pack<float, 4>*>(state) = v;
+                } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (n0 + i < N) state[i] = h[u][i];
+                    for (int i = 0; i < 4; ++i)
+                        if (n0 + i < N) state[i] = h[u][i];
+                }
             }
 #pragma unroll
             for (int m = 1; m < Q; m *= 2) sum += __shfl_xor(sum, m, 64);
-            if (q == 0) {
-                if (p.Dskip) sum = fmaf(p.Dskip[d[u]], x, sum);
-                *y = from_f32<T>(p.z ? sum * silu_f32(z[u]) : sum);
+            if constexpr (WIDE) {
+                const float own = __shfl(sum, lane % kGroup * Q, 64);
+                if (lane / kGroup == u) total[0] = own;
+            } else {
+                total[u] = sum;
             }
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            if (!writer[s]) continue;
+            if (p.Dskip) total[s] = fmaf(skip[s], x[s], total[s]);
+            y[d[s]] = from_f32<T>(p.z ? total[s] * silu_f32(to_f32(gate[s])) : total[s]);
         }
     }
 }
 
-template <typename T, int Q, int U>
-hipError_t launch_step_tiles(const StepParams& p, hipStream_t stream)
+template <typename T, int Q, int U, bool WIDE>
+hipError_t launch_step_conv(const StepParams& p, const dim3 grid, hipStream_t stream)
 {
-    constexpr int kChannels = 256 / Q * U;
-    const dim3 grid((p.dim + kChannels - 1) / kChannels, min(p.batch, kMostRows));
     switch (p.width) {
-        case 0: step_kernel<T, Q, U, 0><<<grid, 256, 0, stream>>>(p); break;
-        case 1: step_kernel<T, Q, U, 1><<<grid, 256, 0, stream>>>(p); break;
-        case 2: step_kernel<T, Q, U, 2><<<grid, 256, 0, stream>>>(p); break;
-        case 3: step_kernel<T, Q, U, 3><<<grid, 256, 0, stream>>>(p); break;
-        case 4: step_kernel<T, Q, U, 4><<<grid, 256, 0, stream>>>(p); break;
+        case 1: step_kernel<T, Q, 1, U, WIDE><<<grid, 256, 0, stream>>>(p); break;
+        case 2: step_kernel<T, Q, 2, U, WIDE><<<grid, 256, 0, stream>>>(p); break;
+        case 3: step_kernel<T, Q, 3, U, WIDE><<<grid, 256, 0, stream>>>(p); break;
+        case 4: step_kernel<T, Q, 4, U, WIDE><<<grid, 256, 0, stream>>>(p); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
 }
-// Blocks of twice the channels where there are several for each place on the machine.
+// MI355X, us, bf16, N = 16.  With the convolution, wide where that has two waves for every SIMD, wide / not: 256 x 4096 39.4 / 46.0, 64 x 4096
+// 11.2 / 12.4, 64 x 1536 6.0 / 5.9, 64 x 768 5.2 / 4.4.  Without it, U = 2 where there are eight blocks for every compute unit,
+// U = 2 / 1: 256 x 4096 25.7 / 27.7, 128 x 1536 8.0 / 8.5, 64 x 1536 4.9 / 5.1, 64 x 768 4.0 / 3.8.
 template <typename T, int Q>
 hipError_t launch_step_lanes(const StepParams& p, hipStream_t stream)
 {
-    const long blocks = (long)p.batch * ((p.dim + 256 / Q - 1) / (256 / Q));
-    return blocks >= 4096 ? launch_step_tiles<T, Q, 2>(p, stream) : launch_step_tiles<T, Q, 1>(p, stream);
+    auto grid = [&](int waves) { return dim3((p.dim + 256 / Q * waves - 1) / (256 / Q * waves), min(p.batch, kMostRows)); };
+    if (p.width == 0) {
+        if ((long)p.batch * grid(1).x >= 2048) step_kernel<T, Q, 0, 2, false><<<grid(2), 256, 0, stream>>>(p);
+        else step_kernel<T, Q, 0, 1, false><<<grid(1), 256, 0, stream>>>(p);
+        return hipGetLastError();
+    }
+    if constexpr (Q == 4)
+        if ((long)p.batch * ((p.dim + 63) / 64) >= 2048) return launch_step_conv<T, Q, Q, true>(p, grid(Q), stream);
+    return launch_step_conv<T, Q, 1, false>(p, grid(1), stream);
 }
 template <typename T>
 hipError_t launch_step_typed(const StepParams& p, hipStream_t stream)
