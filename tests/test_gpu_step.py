@@ -278,3 +278,19 @@ def test_overwritten_tensors_count_their_versions(lb):
         lb.lbscan_step(**t)
     with torch.no_grad():
         lb.lbscan_step(**t)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,D,N,K", [(300, 450, 16, 4), (300, 450, 9, 1), (300, 450, 13, 2), (300, 449, 16, 3), (300, 450, 16, 0), (600, 450, 8, 0),
+                                     (600, 450, 5, 4), (1100, 450, 4, 0), (1100, 300, 3, 4), (2100, 20, 16, 4), (2100, 65, 12, 0)])
+def test_large_steps(lb, dtype, B, D, N, K):
+    """The launches of large calls: rows and channels that no wave divides, a pool with padding and a slot named twice."""
+    t = step_inputs(B, D, N, TYPES[dtype], K=K, S=B + 7)
+    slots = torch.randperm(B + 7, device="cuda", generator=generator(3))[:B].int()
+    slots[B // 2], slots[B - 3], slots[5] = -1, slots[1], B + 7
+    before = {k: t[k].clone() for k in ("state", "conv_state") if k in t}
+    check_step(lb, t, slots=slots)
+    free = torch.ones(B + 7, dtype=torch.bool, device="cuda")
+    free[slots[(slots >= 0) & (slots < B + 7)].long()] = False
+    for k, v in before.items():
+        assert torch.equal(t[k][free], v[free]), k
