@@ -418,6 +418,7 @@ size_t lbscan_block_norm_workspace_bytes(const lbscan_block_norm_args *args);
 /* Softmax cross entropy of tokens over a vocabulary, the product with the table included and the logits never kept:
  *     l[t,v] = scale * sum_d x[t,d] weight[v,d]
  *     lse[t] = log(sum_v exp(l[t,v]))          loss[t] = lse[t] - l[t,targets[t]]
+ * (the loss from the sum relative to the target's term in it: zero or more, also where lse and the logit are large).
  * A token whose target is outside [0, vocab) (padding, a prompt) is left out: its loss, lse and dx are zeros, it has no part in
  * dweight, and its row of x is not looked at.  Logits, maxima and sums are fp32.  The gradients are
  *     G[t,v] = (dloss[t] + dlse[t]) exp(l[t,v] - lse[t]) - dloss[t] (v == targets[t])

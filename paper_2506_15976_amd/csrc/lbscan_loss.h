@@ -43,7 +43,7 @@ struct LossTiles {
     const float* down;                // (rows) fp32: g; bf16: the rounded slope at the target
     const int *tokens_of, *slot;      // bf16, dweight: tokens of each row of the table, and its place in the list
     const void* list;                 // (.., dimp) sums of rest_t x_t
-    float* own;                       // (rows) l of the target
+    float* own;                       // (rows) x_t . W_target
     float2* part;                     // (chunks, live rows) maximum and sum of a chunk of the vocabulary
     float* acc;                       // (splits, live rows, dimp)
     float* share;                     // (splits, count in whole tiles, dimp)

@@ -271,11 +271,15 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2)
     s = s * fast_exp2(m - base) + s2 * fast_exp2(m2 - base);
     m = top;
 }
-// lse and loss of TOKENS tokens a block, 256 / TOKENS threads to each.
+// lse and loss of TOKENS tokens a block, 256 / TOKENS threads to each.  With m and s the maximum and sum to base 2 and e the target's
+// exponent, computed as the sum's terms are (rounded once, in the difference with m), loss = log2(s 2^-e) ln2.  Near the maximum
+// that is the logarithm of the ratio of the sum to the target's own term in it: at least one, and one where there is nothing
+// else, so that a certain token's loss is zero or more and as exact as the sum is, whatever the logits' size (from lse - l it was off by
+// some 2^-24 of |l|).  Farther away the term may vanish, and the difference of the logarithms is at least ln2.
 template <int TOKENS>
 __global__ __launch_bounds__(256) void loss_join_kernel(const float2* __restrict__ part, const float* __restrict__ own,
                                                         const int* __restrict__ rank, float* __restrict__ loss, float* __restrict__ lse,
-                                                        long tokens, int vtiles, const LossChoice* __restrict__ choice)
+                                                        long tokens, int vtiles, const LossChoice* __restrict__ choice, float scale2)
 {
     constexpr int kPieces = 256 / TOKENS;
     const long rows = choice->rows, chunks = loss_ceil(vtiles, choice->chunk_lse);
@@ -303,9 +307,14 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const float2* __restrict
         }
         if (piece == 0 && t < tokens) {
             for (int k = 1; k < 8; ++k) join(m, s, folds[k][at].x, folds[k][at].y);
-            const float v = r >= 0 ? (m + fast_log2(s)) * kLn2 : 0.0f;
-            lse[t] = v;
-            loss[t] = r >= 0 ? v - own[r] : 0.0f;
+            float all = 0.0f, mine = 0.0f;
+            if (r >= 0) {
+                const float e = fmaf(own[r], scale2, -m);
+                all = (m + fast_log2(s)) * kLn2;
+                mine = (e > -1.0f ? fast_log2(s / fast_exp2(e)) : fast_log2(s) - e) * kLn2;
+            }
+            lse[t] = all;
+            loss[t] = mine;
         }
         __syncthreads();
     }
@@ -471,10 +480,11 @@ hipError_t forward(const LossParams& p, const LossPlan& plan, const Scratch& s, 
     e = (sizeof(T) == 4 ? launch_loss_tiles_f32 : launch_loss_tiles_bf16)(LossKind::lse, t, plan.few, plan.loose, stream);
     if (e != hipSuccess) return e;
     const int vtiles = (int)loss_ceil(p.vocab, plan.few ? loss_few_vocab(plan.loose, sizeof(T)) : kLossTile);
+    const float scale2 = p.scale * kLog2e;
     if (plan.few) loss_join_kernel<4><<<some((p.tokens + 3) / 4), 256, 0, stream>>>(t.part, t.own, s.at<int>(plan.rank), p.loss, p.lse, p.tokens,
-                                                                                  vtiles, t.choice);
+                                                                                  vtiles, t.choice, scale2);
     else loss_join_kernel<16><<<some((p.tokens + 15) / 16), 256, 0, stream>>>(t.part, t.own, s.at<int>(plan.rank), p.loss, p.lse, p.tokens, vtiles,
-                                                                            t.choice);
+                                                                            t.choice, scale2);
     return hipGetLastError();
 }
 
