@@ -143,14 +143,16 @@ inline void set_python_error(const Failure& e)
 
 // A backward pass that is being recorded into a graph, and whose next node adds up a leaf's gradient on the default stream, where
 // an eager graph that still lives has left it: torch would make the default stream wait for the recorded one, which ends
-// the recording, or the process, from a thread that no caller sees.
+// the recording, or the process, from a thread that no caller sees.  (It makes no stream wait for nodes that the pass does not
+// reach: other leaves may be in use elsewhere.)
 inline void refuse_leaves_of_the_default_stream()
 {
     const auto node = torch::autograd::get_current_node();
     if (!node) return;
-    for (const auto& edge : node->next_edges()) {
-        if (!edge.function) continue;
-        const auto leaf = edge.function->stream();
+    const auto& edges = node->next_edges();
+    for (size_t k = 0; k < edges.size(); ++k) {
+        if (!edges[k].function || !node->task_should_compute_output(k)) continue;
+        const auto leaf = edges[k].function->stream();
         if (!leaf || leaf->device_type() != c10::DeviceType::CUDA) continue;
         const c10::impl::VirtualGuardImpl guard(leaf->device_type());
         hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
