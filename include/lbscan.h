@@ -325,7 +325,7 @@ size_t lbscan_embed_workspace_bytes(const lbscan_embed_args *args);
  *     y = (sum_n Cm[b,n] state[s,d,n] + Dskip x') SiLU?(z)
  * Both states are updated in place; conv_state holds the last K-1 inputs, oldest first.  Row b has the states at
  * s = slots[b] of the pools, or at b without slots.  A row whose slot is outside [0, pool), or that an earlier row has already, is
- * padding: its y is zeros and no state is touched for it. */
+ * padding: its y is zeros and no state is touched for it.  The states, too, overlap neither inputs nor y nor each other. */
 typedef struct lbscan_step_args {
     int32_t batch, dim, dstate;   /* B, D, N in 1 .. LBSCAN_MAX_DSTATE; B or D may be 0.  B * D <= 2^31 - 4096;
                                      B <= 65536 with slots */
@@ -357,7 +357,8 @@ int lbscan_step(const lbscan_step_args *args, void *hip_stream);
 /* lbscan_conv1d_fwd for sequences that come in pieces (a prompt, its parts, single tokens with seqlen 1): the K-1 tokens
  * before the piece are taken from the state, which is updated in place and holds the last K-1 inputs, oldest first.
  * lengths[b], held to 0 .. L: tokens of row b that are there (a padded batch); y is zero behind them and x is not read, and the
- * state leaves as it is after the last of them.  slots and pool as in lbscan_step; a row of padding has zeros in y. */
+ * state leaves as it is after the last of them.  slots and pool as in lbscan_step; a row of padding has zeros in y.  The
+ * state, too, overlaps neither inputs nor y. */
 typedef struct lbscan_conv_state_args {
     int32_t batch, dim, seqlen;   /* B, D, L; any may be 0 (the state stays).  D * L <= 2^31 - 4096; B <= 65536 with
                                      slots */

@@ -17,19 +17,39 @@ int64_t expect_rows(const char* name, const Tensor& t, int64_t B, int64_t n, at:
     return dense || B <= 1 ? 0 : t.stride(0);
 }
 
-// An output of the caller's must not have memory of an input, which other blocks may still have to read.
-std::pair<uintptr_t, uintptr_t> extent(const Tensor& t)
+// What a call writes to (an output or a state of the caller's) must not have memory of what it reads, or writes besides: other blocks
+// may still have to read it.  A tensor that is written is dense; one that is read is, too, or has rows that may be columns of a wider
+// tensor.
+struct Memory {
+    const char* name;
+    uintptr_t begin = 0, end = 0;                  // the same where there is nothing
+    uintptr_t row = 0, pitch = 0;                  // bytes of a row, and from one to the next; 0: dense
+    Memory(const char* n, const Tensor& t) : name(n)
+    {
+        if (t.numel() == 0) return;
+        begin = reinterpret_cast<uintptr_t>(t.data_ptr());
+        if (t.is_contiguous()) {
+            end = begin + t.nbytes();
+        } else {
+            row = t.size(1) * t.element_size();
+            pitch = t.stride(0) * t.element_size();
+            end = begin + (t.size(0) - 1) * pitch + row;
+        }
+    }
+    Memory(const char* n, const Maybe& t) : name(n) { if (t) *this = Memory(n, *t); }
+};
+void expect_apart(const Memory& written, at::ArrayRef<Memory> others)
 {
-    int64_t last = 0;
-    for (int64_t k = 0; k < t.dim(); ++k) last += (t.size(k) - 1) * t.stride(k);
-    const auto first = reinterpret_cast<uintptr_t>(t.data_ptr());
-    return {first, first + (last + 1) * t.element_size()};
-}
-void expect_apart(const Maybe& out, const Maybe& input, const char* name)
-{
-    if (!out || !input || !out->numel() || !input->numel()) return;
-    const auto a = extent(*out), b = extent(*input);
-    if (a.first < b.second && b.first < a.second) throw Failure(LBSCAN_EINVAL, std::string("out must not be, or share memory with, ") + name);
+    if (written.begin == written.end) return;
+    for (const Memory& o : others) {
+        if (o.begin == o.end || o.begin >= written.end || written.begin >= o.end) continue;
+        if (o.pitch && written.begin >= o.begin) {
+            // between two rows: behind the one that begins before it, in front of the next
+            const uintptr_t from = (written.begin - o.begin) % o.pitch;
+            if (from >= o.row && from + (written.end - written.begin) <= o.pitch) continue;
+        }
+        throw Failure(LBSCAN_EINVAL, std::string(written.name) + " must not be, or share memory with, " + o.name);
+    }
 }
 
 // A pool of states, and the rows' places in it.
@@ -84,14 +104,12 @@ Tensor step(Tensor x, Tensor delta, Tensor A, Tensor Bm, Tensor Cm, Tensor state
     const Stream stream(stream_object, x);
     expect("out", out, {B, D}, type, x);
     expect_writable("out", out);
-    if (out) {
-        using Named = std::pair<const Maybe, const char*>;
-        for (const auto& [t, name] : {Named{x, "x"}, Named{delta, "delta"}, Named{z, "z"}, Named{Bm, "Bm"}, Named{Cm, "Cm"}, Named{A, "A"},
-                                      Named{state, "state"}, Named{conv_state, "conv_state"}, Named{Dskip, "Dskip"},
-                                      Named{delta_bias, "delta_bias"}, Named{conv_weight, "conv_weight"}, Named{conv_bias, "conv_bias"},
-                                      Named{slots, "slots"}})
-            expect_apart(out, t, name);
-    }
+    const Memory states("state", state), conv_states("conv_state", conv_state);
+    const Memory inputs[] = {{"x", x}, {"delta", delta}, {"z", z}, {"Bm", Bm}, {"Cm", Cm}, {"A", A}, {"Dskip", Dskip},
+                             {"delta_bias", delta_bias}, {"conv_weight", conv_weight}, {"conv_bias", conv_bias}, {"slots", slots}};
+    for (const Memory& written : {Memory("out", out), states, conv_states}) expect_apart(written, inputs);
+    expect_apart({"out", out}, {states, conv_states});
+    expect_apart(states, {conv_states});
     Tensor y = out ? *out : fresh(stream, {B, D}, x, type);
     a.batch = size32("x", B);
     a.dim = size32("x", D);
@@ -139,12 +157,10 @@ Tensor conv1d_prompt(Tensor x, Maybe state, Tensor weight, Maybe bias, bool acti
     const Stream stream(stream_object, x);
     expect("out", out, x.sizes(), type, x);
     expect_writable("out", out);
-    expect_apart(out, x, "x");
-    expect_apart(out, state, "state");
-    expect_apart(out, weight, "weight");
-    expect_apart(out, bias, "bias");
-    expect_apart(out, lengths, "lengths");
-    expect_apart(out, slots, "slots");
+    const Memory states("state", state);
+    const Memory inputs[] = {{"x", x}, {"weight", weight}, {"bias", bias}, {"lengths", lengths}, {"slots", slots}};
+    for (const Memory& written : {Memory("out", out), states}) expect_apart(written, inputs);
+    expect_apart({"out", out}, {states});
     Tensor y = out ? *out : fresh(stream, x.sizes(), x, type);
     a.batch = size32("x", B);
     a.dim = size32("x", D);
@@ -207,11 +223,8 @@ BlockNormResult block_norm_run(const BlockNorm& n, bool stats, const Maybe& out,
     c10::DeviceGuard guard(x.device());
     expect("out", out, x.sizes(), x.scalar_type(), x);
     expect_writable("out", out);
-    expect_apart(out, x, "x");
-    expect_apart(out, n.gate, "the gate");
-    expect_apart(out, n.residual, "the residual");
-    expect_apart(out, n.weight, "weight");
-    expect_apart(out, n.branch_weight, "branch_weight");
+    expect_apart({"out", out}, {{"x", x}, {"the gate", n.gate}, {"the residual", n.residual}, {"weight", n.weight},
+                                {"branch_weight", n.branch_weight}});
     BlockNormResult r;
     r.y = out ? *out : fresh(stream, x.sizes(), x, x.scalar_type());
     if (n.residual) r.sum = fresh(stream, x.sizes(), x, at::kFloat);

@@ -10,7 +10,8 @@ are before they are used on another.  Outputs and scratch are that stream's memo
 current one.
 
 out, and the states of steps and prompts, are overwritten as in-place operations overwrite: autograd sees it by their versions, and
-tensors that require gradients are refused while gradients are recorded."""
+tensors that require gradients are refused while gradients are recorded.  Of steps and prompts of the scan and its convolution, and of
+the norms around a block, they share no memory with what the call reads or writes besides (refused)."""
 from __future__ import annotations
 
 import importlib.util
