@@ -449,7 +449,6 @@ LossTiles tiles_of(const LossParams& p, const LossPlan& plan, const Scratch& s)
     t.w = plan.copy_weight ? s.at<void>(plan.w) : p.weight;
     t.x = s.at<void>(plan.x);
     t.targets = s.at<int>(plan.targets);
-    t.rows = plan.rows;
     t.vocab = p.vocab; t.dim = p.dim; t.dimp = plan.dimp; t.ldw = plan.loose ? p.dim : plan.dimp; t.piece = plan.piece;
     t.first = 0; t.count = p.vocab;
     t.last = 1;

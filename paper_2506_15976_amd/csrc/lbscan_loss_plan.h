@@ -105,7 +105,8 @@ inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool 
     const int ntile = loss_tokens(p.few, element), wtile = loss_tokens(0, element), units = loss_units(p.few, p.loose, element);
     p.rows = loss_ceil(tokens, ntile) * ntile;
     const long mtiles = loss_ceil(p.dimp, kLossTile), vtiles = loss_ceil(vocab, kLossTile);
-    // G: at most a gigabyte of the vocabulary at a time, in pieces that are just a whole number of rounds of dweight's tiles
+    // G: a gigabyte of the vocabulary at a time, in pieces that are just a whole number of rounds of dweight's tiles; one tile of
+    // 256 columns where that is more (from 2^21 tokens in bf16, 2^20 in fp32; 8 and 16 GiB of 2^24 tokens)
     long most = ((long)1 << 30) / (p.rows * element) / kLossTile;
     if (most < 1) most = 1;
     long tiles = vtiles;
@@ -146,7 +147,8 @@ inline LossPlan loss_plan_of(long tokens, int vocab, int dim, int element, bool 
             }
         }
         if (want_dx) {
-            // as many parts as all tokens need, and more for fewer live ones
+            // as many parts as all tokens need, and more for fewer live ones: room for 8192 rows at the least (192 MiB of 6144 columns, 2 GiB
+            // of 65536), 1024 of few tokens
             const long few_rows = p.few ? 1024 : 8192;
             p.acc_rows = p.rows * loss_best_splits(loss_ceil(p.dimp, p.few ? loss_few_vocab(p.loose, element) : kLossTile) * (p.rows / ntile), (int)loss_ceil(p.piece, step), units, element);
             if (p.acc_rows < few_rows) p.acc_rows = few_rows;

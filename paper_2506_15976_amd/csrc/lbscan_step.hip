@@ -33,8 +33,8 @@ __device__ __forceinline__ float silu_f32(float v) { return v * sigmoid_f32(v); 
 // whose lanes all compute what a channel has one of.  Everything is loaded before the search for an earlier row with the same slot
 // ends: only what is stored waits for it.  Loads of the optional inputs stand in branches, where a sum or a conversion would wait for
 // all loads before it: those come later (256 x 4096 without the convolution 34.2 -> 25.3 us).  Bound by memory, read and written in
-// the same places: MI355X, 256 x 4096 x 16 bf16 with the convolution, states in a pool (155.6 MB) 39.4 us (3.9 TB/s), without it 25.7
-// (5.5 TB/s; a sum in place of that size 26.0).
+// the same places: MI355X, three sets of inputs in turn, 256 x 4096 x 16 bf16 with the convolution, states in a pool (155.6 MB) 41.2 us
+// (3.8 TB/s; two sets, part of which the last cache keeps, 36.9), without it 25.1 (5.7 TB/s).
 template <typename T, int Q, int K, int U, bool WIDE>
 __global__ __launch_bounds__(256) void step_kernel(const StepParams p)
 {
@@ -187,8 +187,8 @@ hipError_t launch_step_conv(const StepParams& p, const dim3 grid, hipStream_t st
     }
     return hipGetLastError();
 }
-// MI355X, us, bf16, N = 16.  With the convolution, wide where that has two waves for every SIMD, wide / not: 256 x 4096 39.4 / 46.0, 64 x 4096
-// 11.2 / 12.4, 64 x 1536 6.0 / 5.9, 64 x 768 5.2 / 4.4.  Without it, U = 2 where there are eight blocks for every compute unit,
+// MI355X, us, bf16, N = 16.  With the convolution, three sets of inputs in turn, in a graph, wide where that has two waves for every SIMD, wide /
+// not: 256 x 4096 41.3 / 47.0, 64 x 4096 11.7 / 13.6, 64 x 1536 6.5 / 5.7, 64 x 768 5.0 / 4.3.  Without it, U = 2 where there are eight blocks for every compute unit,
 // U = 2 / 1: 256 x 4096 25.7 / 27.7, 128 x 1536 8.0 / 8.5, 64 x 1536 4.9 / 5.1, 64 x 768 4.0 / 3.8.
 template <typename T, int Q>
 hipError_t launch_step_lanes(const StepParams& p, hipStream_t stream)
